@@ -56,7 +56,7 @@ typedef enum {
     VT_ERR_DEVICE = 6     /* a HIP call failed (launch error, no device) */
 } vt_status;
 
-typedef enum { VT_F32 = 0, VT_BF16 = 1 } vt_dtype;
+typedef enum { VT_F32 = 0, VT_BF16 = 1, VT_E4M3 = 2 /* of a key-value cache only, see vocabtrim_attention.h */ } vt_dtype;
 typedef enum { VT_I32 = 0, VT_I64 = 1 } vt_itype;
 
 /* Largest m (tokens kept per hidden row) vt_draft_head_step accepts. */

@@ -1,4 +1,5 @@
-"""Thin Python binding over the C ABI of libvocabtrim.so (include/vocabtrim.h).
+"""Thin Python binding over the C ABI of libvocabtrim.so (include/vocabtrim.h; attention.py has that of
+include/vocabtrim_attention.h).
 
 Argument marshalling only: torch tensors supply device memory and the current
 HIP stream; every step of the path runs in the library's kernels.  There is no
@@ -29,6 +30,8 @@ EXPORTS = (
     "vt_draft_head_step_static", "vt_draft_head_step_plan", "vt_draft_head_step_multi_plan",
     "vt_tree_expand", "vt_tree_rerank", "vt_draft_tree_level", "vt_stream_read_reference",
     "vt_build_trimmed_heads", "vt_draft_head_step_multi", "vt_draft_head_step_multi_ws_bytes",
+    "vt_qk_norm_rope", "vt_qk_norm_rope_backward", "vt_qk_norm_rope_backward_ws_bytes",
+    "vt_qkv_to_cache", "vt_kv_cache_read", "vt_paged_attention", "vt_paged_attention_ws_bytes",
 )
 VT_MAX_HEADS, VT_MULTI_MAX_ROWS = 16, 256
 VT_TREE_MAX_CANDIDATES, VT_TREE_MAX_KEEP = 16384, 1024
@@ -91,6 +94,22 @@ def load_library() -> ctypes.CDLL:
     L.vt_draft_head_step_multi.restype = ci
     L.vt_draft_head_step_multi_ws_bytes.argtypes = [i32, i32, vp, i32, i32]
     L.vt_draft_head_step_multi_ws_bytes.restype = sz
+    f32 = ctypes.c_float
+    norm = [ci, i64, i32, i32, i32, vp, vp, f32, vp, i64, i32, ci, vp, ci]      # type, n, head counts and size, weights, table, positions
+    L.vt_qk_norm_rope.argtypes = [vp, i64, vp, i64, *norm, vp, i64, vp, i64, vp]
+    L.vt_qk_norm_rope.restype = ci
+    L.vt_qk_norm_rope_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, *norm, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    L.vt_qk_norm_rope_backward.restype = ci
+    L.vt_qk_norm_rope_backward_ws_bytes.argtypes = [i64, i32]
+    L.vt_qk_norm_rope_backward_ws_bytes.restype = sz
+    L.vt_qkv_to_cache.argtypes = [vp, i64, vp, i64, vp, i64, ci, i64, i32, vp, vp, f32, vp, i64, i32, ci, vp, ci, vp, i64, vp, vp, ci, vp]
+    L.vt_qkv_to_cache.restype = ci
+    L.vt_kv_cache_read.argtypes = [vp, vp, ci, i64, vp, vp, ci, vp]
+    L.vt_kv_cache_read.restype = ci
+    L.vt_paged_attention.argtypes = [vp, i64, ci, i64, i32, vp, vp, i32, vp, i32, vp, i32, vp, i64, f32, vp, i64, vp, vp, sz, vp]
+    L.vt_paged_attention.restype = ci
+    L.vt_paged_attention_ws_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i64]
+    L.vt_paged_attention_ws_bytes.restype = sz
     _connect(L)
     _lib = L
     return L

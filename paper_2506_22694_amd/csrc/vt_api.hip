@@ -8,6 +8,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "vt_attn.h"
 #include "vt_build.h"
 #include "vt_step.h"
 #include "vt_tree.h"
@@ -777,6 +778,10 @@ const StepShape &step_shape(int n, int k, int d, int m, int dtype) {
 int step_chunk(int n, int k, int d, int m, int dtype) { return step_shape(n, k, d, m, dtype).chunk; }
 
 }  // namespace
+
+namespace vt {
+int status_of_hip(hipError_t e) { return device_status(e); }
+}  // namespace vt
 
 extern "C" {
 

@@ -1,0 +1,57 @@
+// Where a paged cache's rows lie, for the kernels that write and read them.  No HIP in here: what arrives in device memory (slots,
+// page numbers, lengths) is checked by these functions alone, and the tests run them on the host.
+#pragma once
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define VT_BOTH __host__ __device__ __forceinline__
+#else
+#define VT_BOTH inline
+#endif
+
+namespace vt {
+
+// Index of a head's row in [pages, heads, page_size], or -1 for a slot outside the cache.
+VT_BOTH int64_t row_of_slot(int64_t slot, int64_t pages, int heads, int head, int page_shift) {
+    if (slot < 0 || (slot >> page_shift) >= pages) return -1;
+    const int64_t place = slot & (((int64_t)1 << page_shift) - 1);
+    return ((((slot >> page_shift) * heads) + head) << page_shift) + place;
+}
+// Index of a head's first row in a page, or -1 for a page outside the cache.
+VT_BOTH int64_t row_of_page(int page, int64_t pages, int heads, int head, int page_shift) {
+    if (page < 0 || page >= pages) return -1;
+    return ((int64_t)page * heads + head) << page_shift;
+}
+// Cached tokens of a request that are looked at.
+VT_BOTH int tokens_of(int length, int64_t most) { return length < 0 ? 0 : length > most ? (int)most : length; }
+
+// New rows of request b: the first one in `first`; none where row_start is out of order or past the n rows there are.
+VT_BOTH int rows_of(const int32_t *row_start, int b, int64_t n, int max_rows, int64_t &first) {
+    if (row_start == nullptr) {
+        first = b;
+        return 1;
+    }
+    first = row_start[b];
+    int64_t end = row_start[b + 1];
+    if (end > n) end = n;
+    if (first < 0 || end <= first) return 0;
+    return end - first > max_rows ? max_rows : (int)(end - first);
+}
+
+// A request's tokens are cut into equal pieces of whole tiles, one for each of its workgroups: `splits` of them at most, and no piece
+// below `least` tokens, so that short requests among long ones do not pay for pieces that hold next to nothing.
+VT_BOTH int piece_tokens(int tokens, int splits, int least) {
+    int piece = (int)(((int64_t)tokens + splits - 1) / splits);
+    piece = (piece + least - 1) / least * least;
+    return piece < least ? least : piece;
+}
+VT_BOTH int pieces_of(int tokens, int piece) { return tokens <= piece ? 1 : (tokens - 1) / piece + 1; }
+
+// Exponent (biased by 127) of the smallest power of two 2^e, e >= -126, with amax <= 448 * 2^e, from the bits of a finite amax >= 0:
+// 448 = 1.75 * 2^8.
+VT_BOTH int scale_exponent(uint32_t amax_bits) {
+    const int e = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e < 1 ? 1 : e;
+}
+
+}  // namespace vt
