@@ -25,6 +25,7 @@ extern "C" {
 
 #define VT_MAX_HEAD_DIM 256
 #define VT_MAX_ATTENTION_HEADS 1024
+#define VT_MAX_REQUESTS 65535
 
 /* ------------------------------------------------------------------------
  * Norm and rotation.  For every head x in R^head_dim of q (and k likewise):
@@ -129,7 +130,7 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *   q, out       [n, q_heads, head_dim], type VT_BF16 or VT_F32; n <= n_requests * max_rows
  *   page_table   [n_requests, table_pages] int32; entries past a request's tokens are
  *                not used.  Tokens of a page outside [0, cache->pages) are not seen.
- *   lengths      [n_requests] int32; below 0 counts as 0, above
+ *   lengths      [n_requests] int32, n_requests <= VT_MAX_REQUESTS; below 0 counts as 0, above
  *                min(max_length, table_pages * page_size) as that
  *   row_start    [n_requests + 1] int32: rows row_start[b] .. row_start[b + 1] - 1 are
  *                request b's, at most max_rows of them (more are not computed);

@@ -4,61 +4,99 @@
 namespace vt {
 namespace {
 
-constexpr int kJoinWaves = 4;
+constexpr int kJoinThreads = 256;
 
-// One wave to a row and head: the pieces' sums, each brought to the maximum of all.  A piece's sum of 0 has nothing of the row.
-template <bool F32Q>
-__global__ __launch_bounds__(64 * kJoinWaves) void attend_join_kernel(AttendArgs a) {
-    const int lane = lane_id();
-    const int64_t i = (int64_t)blockIdx.x * kJoinWaves + (threadIdx.x >> 6);      // (request, row of it, head)
-    const int head = (int)(i % a.hq), r = (int)(i / a.hq % a.max_rows);
-    const int64_t b = i / a.hq / a.max_rows;
-    if (b >= a.requests) return;
-    int64_t first;
-    if (r >= rows_of(a.row_start, (int)b, a.n, a.max_rows, first)) return;
-    const int len = tokens_of(a.lengths[b], a.most);
-    const int pieces = pieces_of(len, piece_tokens(len, a.splits, kAttendLeast));
-    if (pieces == 1) return;
-    const int64_t at = ((first + r) * a.hq + head) * a.splits;
-    float top = kNone;
-    for (int s = lane; s < pieces; s += 64) top = fmaxf(top, a.part_ms[at + s].x);
-    top = wave_max(top);
-    const int d = 4 * lane;
-    float total = 0.0f, o[4] = {};
-    for (int s0 = 0; s0 < pieces; s0 += 64) {
-        const float2 ms = a.part_ms[at + min(s0 + lane, pieces - 1)];
-        const float f = ms.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ms.x - top);
-        const float part = ms.y == 0.0f ? 0.0f : ms.y * f;
-        const int here = min(64, pieces - s0);
-#pragma unroll 4
-        for (int s = 0; s < here; ++s) {
-            const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-            total += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(part), s));
-            float x[4] = {};
-            if (d < a.cache.D) F32::load4(a.part_o + (at + s0 + s) * a.cache.D + d, x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] += x[j] * fs;
-        }
+// One workgroup to a row and head of a request that several workgroups had parts of: their sums, each brought to the maximum of all; a
+// part's sum of 0 has nothing of the row.  LV lanes read a part's row, so that the workgroup has 256 / LV parts in flight at a time (a wave
+// for all of them, one after the other: 18.6 us for 32 heads of 128 parts).
+template <int LV, bool F32Q>
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a) {
+    constexpr int GROUPS = kJoinThreads / LV;
+    __shared__ __align__(16) float sums[GROUPS][4 * LV];
+    __shared__ float totals[GROUPS];
+    const int head = blockIdx.y;
+    int b = blockIdx.x, r = 0;
+    if (a.max_rows > 1) {
+        r = b % a.max_rows;
+        b /= a.max_rows;
     }
-    if (d < a.cache.D) finish_row(a, first + r, head, d, o, top, total, F32Q);
+    const int4 parts = a.part_at[b];
+    int64_t first;
+    if (r >= rows_of(a.row_start, b, a.n, a.max_rows, first) || parts.y == 1) return;
+    const int h = head / a.G, rows = 16 * a.row_tiles, x = r * a.G + head - h * a.G, rb = x / rows;
+    const int64_t at = ((int64_t)(rb * a.cache.heads + h) * a.places + parts.x) * 2 * rows + (x - rb * rows);
+    // part i: of place parts.x + i, there the first one but for a request that begins within a share
+    auto index = [&](int i) { return at + (int64_t)(2 * i + (i == 0 ? parts.z : 0)) * rows; };
+    const int lane = lane_id(), group = threadIdx.x / LV, d = 4 * (threadIdx.x % LV);
+    const int from = d < a.cache.D ? d : 0;
+    constexpr int AHEAD = 4;      // parts of a group that are asked for along with the maxima
+    float2 ms[AHEAD];
+    float v[AHEAD][4];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        const int64_t k = index(min(group + i * GROUPS, parts.y - 1));
+        ms[i] = a.part_ms[k];
+        F32::load4(a.part_o + k * a.cache.D + from, v[i]);
+    }
+    float top = kNone;
+    for (int s = lane; s < parts.y; s += 64) top = fmaxf(top, a.part_ms[index(s)].x);
+    top = wave_max(top);
+    float total = 0.0f, o[4] = {};
+    auto add = [&](int s, float2 part, const float *u) {
+        const bool nothing = s >= parts.y || part.y == 0.0f;
+        const float f = __builtin_amdgcn_exp2f(part.x - top);
+        total += nothing ? 0.0f : part.y * f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += nothing ? 0.0f : u[j] * f;
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) add(group + i * GROUPS, ms[i], v[i]);
+#pragma unroll 4
+    for (int s = group + AHEAD * GROUPS; s < parts.y; s += GROUPS) {
+        float u[4];
+        F32::load4(a.part_o + index(s) * a.cache.D + from, u);
+        add(s, a.part_ms[index(s)], u);
+    }
+    F32::store4(&sums[group][d], o);
+    if (d == 0) totals[group] = total;
+    __syncthreads();
+    if (group != 0 || d >= a.cache.D) return;
+#pragma unroll
+    for (int s = 1; s < GROUPS; ++s) {
+        total += totals[s];
+        float v[4];
+        F32::load4(&sums[s][d], v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += v[j];
+    }
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] *= inverse;
+    store_values(a, (first + r) * a.out_stride + head * a.cache.D + d, o, F32Q);
+    if (d == 0 && a.lse != nullptr) a.lse[(first + r) * a.hq + head] = log_sum_exp(top, total);
+}
+
+template <int LV>
+void run_join(const AttendArgs &a, bool f32, hipStream_t st) {
+    const dim3 grid((unsigned)(a.requests * a.max_rows), (unsigned)a.hq);
+    if (f32) attend_join_kernel<LV, true><<<grid, kJoinThreads, 0, st>>>(a);
+    else attend_join_kernel<LV, false><<<grid, kJoinThreads, 0, st>>>(a);
 }
 
 }  // namespace
 
 int attend_row_tiles(int rows, int D, bool f32) {
-    if (f32 || rows <= 16) return 1;
-    if (rows <= 32 || D > 64) return D > 128 ? 1 : 2;
-    return 4;
+    if (f32 || rows <= 16 || D > 128) return 1;
+    return rows <= 32 || D > 64 ? 2 : 4;
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool f32, hipStream_t st) {
-    const int D = a.cache.D, tiles = attend_row_tiles(a.max_rows * a.G, D, f32);
+    const int D = a.cache.D, tiles = a.row_tiles;
     hipError_t e = D <= 64 ? launch_attend_d64(a, tiles, f32, st) : D <= 128 ? launch_attend_d128(a, tiles, f32, st) : launch_attend_d256(a, tiles, f32, st);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t waves = (int64_t)a.requests * a.max_rows * a.hq;
-    const unsigned grid = (unsigned)((waves + kJoinWaves - 1) / kJoinWaves);
-    if (f32) attend_join_kernel<true><<<grid, 64 * kJoinWaves, 0, st>>>(a);
-    else attend_join_kernel<false><<<grid, 64 * kJoinWaves, 0, st>>>(a);
+    if (e != hipSuccess || a.whole) return e;
+    if (D <= 64) run_join<16>(a, f32, st);
+    else if (D <= 128) run_join<32>(a, f32, st);
+    else run_join<64>(a, f32, st);
     return hipGetLastError();
 }
 

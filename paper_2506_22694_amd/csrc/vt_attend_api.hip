@@ -59,41 +59,48 @@ vt::CacheArgs cache_args(const vt_kv_cache &c) {
     return {c.k, c.v, coded ? c.k_scale : nullptr, coded ? c.v_scale : nullptr, c.pages, c.heads, __builtin_ctz((unsigned)c.page_size), c.head_dim};
 }
 
-// How attention is cut up: row blocks of a kv head's query rows, and pieces of a request's tokens.
+// How attention is cut up: blocks of a kv head's query rows, and shares of all requests' tokens.
 struct Split {
-    bool ok = false;
-    int row_blocks = 1, splits = 1;
-    size_t bytes = 0, most_bytes = 0;      // of this call; of any call of up to these sizes
+    bool ok = false, whole = true;
+    int row_blocks = 1, row_tiles = 1, places = 1;
+    size_t entries = 0, bytes = 0, most_bytes = 0;       // rows of partial results; bytes of this call; of any call of up to these sizes
 };
-// Workgroups that keep the card's memory busy: four on each of its 256 CUs.
-constexpr int64_t kAttendWorkgroups = 1024;
-constexpr int kMaxSplits = 256;
+
+// Shares that all requests' tokens are cut into: two workgroups' on each of the 256 CUs, all there at a time.  With half as many the ragged
+// 8-bit batch takes 107 us instead of 104 and 131001 tokens of one request 88.0 instead of 88.8; with twice as many 106 and 92.
+constexpr int64_t kAttendWorkgroups = 512;
+// Up to here a workgroup takes a request whole, without the second launch: 300 tokens 6.6 us whole, 7.9 in shares; 512 tokens 8.9 and 8.0.
+constexpr int64_t kAttendWhole = 384;
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32) {
     Split s;
     if (n < 0 || n >= kMaxRows || q_heads < 1 || q_heads > VT_MAX_ATTENTION_HEADS || kv_heads < 1 || q_heads % kv_heads != 0 || D < 16 || D > VT_MAX_HEAD_DIM ||
-        requests < 0 || max_rows < 1 || n > (int64_t)requests * max_rows || max_length < 0 || max_length > kMaxLength)
+        requests < 0 || requests > VT_MAX_REQUESTS || max_rows < 1 || n > (int64_t)requests * max_rows || max_length < 0 || max_length > kMaxLength)
         return s;
     const int64_t rows = (int64_t)max_rows * (q_heads / kv_heads);
-    if (rows > kMaxLength) return s;
-    const int per = 16 * vt::attend_row_tiles((int)rows, D, f32);
-    const int64_t blocks = (rows + per - 1) / per, units = requests * kv_heads * blocks;
-    if (units > kMaxGrid || (int64_t)requests * max_rows * q_heads > kMaxGrid) return s;
-    const int64_t most = (max_length + vt::kAttendLeast - 1) / vt::kAttendLeast;
-    int64_t splits = units == 0 ? 1 : (kAttendWorkgroups + units - 1) / units;
-    if (splits > most) splits = most;
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    if (splits < 1) splits = 1;
+    const int64_t steps = (max_length + vt::kAttendLeast - 1) / vt::kAttendLeast;
+    // (workgroups and threads of a launch, and all requests' steps, are 32-bit numbers)
+    if (rows > kMaxGrid || (int64_t)requests * max_rows * q_heads > kMaxGrid || (steps + 1) * requests > kMaxLength) return s;
+    s.row_tiles = vt::attend_row_tiles((int)rows, D, f32);
+    const int64_t per = 16 * s.row_tiles, blocks = (rows + per - 1) / per, units = kv_heads * blocks;
+    s.whole = max_length <= kAttendWhole;
+    int64_t places = requests;
+    if (!s.whole) {
+        places = (kAttendWorkgroups + units - 1) / units;
+        if (places > steps * requests) places = steps * requests;
+    }
+    if (places * units > kMaxGrid || places > 65535) return s;
     s.ok = true;
     s.row_blocks = (int)blocks;
-    s.splits = (int)splits;
-    s.bytes = (size_t)n * q_heads * splits * (D * sizeof(float) + 2 * sizeof(float));
-    // What a call of up to these sizes takes: row heads times splits are at most all row heads times the pieces there can be, and
-    // -- splits being below workgroups / units + 1 -- the rows of a unit times the workgroups and all row heads once more.
-    const int64_t all = n * q_heads, pieces = most < kMaxSplits ? most : kMaxSplits, unit = rows < per ? rows : per;
-    const int64_t entries = all * pieces < unit * kAttendWorkgroups + all ? all * pieces : unit * kAttendWorkgroups + all;
-    s.most_bytes = most <= 1 ? 0 : round_up((size_t)entries * (D * sizeof(float) + 2 * sizeof(float)), 256);
-    if (splits == 1) s.bytes = 0;
+    s.places = (int)places;
+    if (s.whole) return s;
+    const size_t entry = (D + 2) * sizeof(float);
+    s.entries = (size_t)units * places * 2 * per;
+    s.bytes = s.entries * entry + requests * sizeof(int4);
+    // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
+    // larger with fewer rows.
+    const size_t most = 2 * (size_t)(kAttendWorkgroups * per + kv_heads * (rows + per));
+    s.most_bytes = round_up(most * entry + requests * sizeof(int4), 256);
     return s;
 }
 
@@ -238,9 +245,11 @@ int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int
     a.most = max_length < held ? max_length : held;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.out = out, a.out_stride = out_stride, a.lse = out_lse;
-    a.splits = split.splits, a.row_blocks = split.row_blocks;
+    a.whole = split.whole, a.places = split.places, a.row_blocks = split.row_blocks, a.row_tiles = split.row_tiles;
+    a.G_magic = (unsigned)(((uint64_t)1 << 32) / a.G) + 1u;
     a.part_o = static_cast<float *>(ws);
-    a.part_ms = reinterpret_cast<float2 *>(static_cast<float *>(ws) + (size_t)n * q_heads * split.splits * cache->head_dim);
+    a.part_ms = reinterpret_cast<float2 *>(a.part_o + split.entries * cache->head_dim);
+    a.part_at = reinterpret_cast<int4 *>(a.part_ms + split.entries);
     return vt::status_of_hip(vt::launch_attend(a, f32, static_cast<hipStream_t>(stream)));
 }
 

@@ -3,10 +3,8 @@
 
 namespace vt {
 
-hipError_t launch_attend_d256(const AttendArgs &a, int tiles, bool f32, hipStream_t st) {
-    if (f32) return run_attend<256, 1, true>(a, st);
-    if (tiles == 1) return run_attend<256, 1, false>(a, st);
-    return run_attend<256, 2, false>(a, st);
+hipError_t launch_attend_d256(const AttendArgs &a, int, bool f32, hipStream_t st) {
+    return f32 ? run_attend<256, 1, true>(a, st) : run_attend<256, 1, false>(a, st);
 }
 
 }  // namespace vt

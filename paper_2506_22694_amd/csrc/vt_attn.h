@@ -66,9 +66,13 @@ struct AttendArgs {
     void *out;
     int64_t out_stride;
     float *lse;
-    int splits, row_blocks;
-    float *part_o;      // [n, hq, splits, D], then [n, hq, splits] (max, sum): with more than one split
+    int row_blocks, row_tiles;      // blocks of 16 row_tiles query rows
+    int whole;                      // a workgroup to each request, kv head and row block
+    int places;                     // ... or this many to all requests together, of each kv head and row block
+    unsigned G_magic;               // floor(2^32 / G) + 1, G > 1
+    float *part_o;                  // [row_blocks, heads, places, 2, 16 row_tiles, D], the same of (max, sum),
     float2 *part_ms;
+    int4 *part_at;                  // [requests]: first place of a request's parts, how many, the first one's number there
 };
 // 16-row tiles of queries that one workgroup takes
 int attend_row_tiles(int rows, int D, bool f32);
@@ -76,7 +80,7 @@ hipError_t launch_attend(const AttendArgs &a, bool f32, hipStream_t st);
 
 constexpr int kAttendWaves = 4;
 constexpr int kAttendTile = 32;                                   // cached tokens that a wave takes at a time
-constexpr int kAttendLeast = kAttendWaves * kAttendTile;          // ... and the least a workgroup is given
+constexpr int kAttendLeast = kAttendWaves * kAttendTile;          // ... and a workgroup: the steps that requests are cut up by
 
 // csrc/vt_attend_d*.hip
 hipError_t launch_attend_d64(const AttendArgs &a, int tiles, bool f32, hipStream_t st);

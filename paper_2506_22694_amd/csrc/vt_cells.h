@@ -38,14 +38,17 @@ VT_BOTH int rows_of(const int32_t *row_start, int b, int64_t n, int max_rows, in
     return end - first > max_rows ? max_rows : (int)(end - first);
 }
 
-// A request's tokens are cut into equal pieces of whole tiles, one for each of its workgroups: `splits` of them at most, and no piece
-// below `least` tokens, so that short requests among long ones do not pay for pieces that hold next to nothing.
-VT_BOTH int piece_tokens(int tokens, int splits, int least) {
-    int piece = (int)(((int64_t)tokens + splits - 1) / splits);
-    piece = (piece + least - 1) / least * least;
-    return piece < least ? least : piece;
+// Requests are taken in steps of `step` tokens; one without tokens has one too, for its rows' results.
+VT_BOTH int steps_of(int tokens, int rows, int step) {
+    return rows <= 0 ? 0 : tokens <= step ? 1 : (int)((unsigned)(tokens - 1) / (unsigned)step) + 1;
 }
-VT_BOTH int pieces_of(int tokens, int piece) { return tokens <= piece ? 1 : (tokens - 1) / piece + 1; }
+// All requests' steps, one after the other, in shares of `per`: the start of share `place`, and its length (0: there is none).
+VT_BOTH int share_steps(int all, int places, int place, int &per, int &start) {
+    per = all <= places ? 1 : (int)((unsigned)(all - 1) / (unsigned)places) + 1;
+    const int64_t from = (int64_t)place * per;
+    start = from < all ? (int)from : all;
+    return all - start < per ? all - start : per;
+}
 
 // Exponent (biased by 127) of the smallest power of two 2^e, e >= -126, with amax <= 448 * 2^e, from the bits of a finite amax >= 0:
 // 448 = 1.75 * 2^8.

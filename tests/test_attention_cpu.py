@@ -125,7 +125,7 @@ def test_attention_refuses(lib):
 
 def test_workspace_for_the_largest_call_serves_all_below(lib):
     size = lib.vt_paged_attention_ws_bytes
-    assert size(1, 32, 8, 128, 1, 1, 128) == 0 and size(1, 32, 7, 128, 1, 1, 1 << 20) == 0 and size(3, 32, 8, 128, 2, 1, 1 << 20) == 0
+    assert size(1, 32, 8, 128, 1, 1, 128) == 0 == size(9, 32, 8, 128, 70000, 1, 1 << 20) and size(1, 32, 7, 128, 1, 1, 1 << 20) == 0 and size(3, 32, 8, 128, 2, 1, 1 << 20) == 0
     import random
     rng = random.Random(3)
     for _ in range(300):
@@ -170,8 +170,8 @@ int64_t slot(int64_t s, int64_t pages, int heads, int head, int shift) { return 
 int64_t page(int p, int64_t pages, int heads, int head, int shift) { return vt::row_of_page(p, pages, heads, head, shift); }
 int tokens(int length, int64_t most) { return vt::tokens_of(length, most); }
 int rows(const int32_t *start, int b, int64_t n, int max_rows, int64_t *first) { return vt::rows_of(start, b, n, max_rows, *first); }
-int piece(int t, int splits, int least) { return vt::piece_tokens(t, splits, least); }
-int pieces(int t, int piece) { return vt::pieces_of(t, piece); }
+int steps(int tokens, int rows, int step) { return vt::steps_of(tokens, rows, step); }
+int share(int all, int places, int place, int *per, int *start) { return vt::share_steps(all, places, place, *per, *start); }
 int exponent(float x) { uint32_t u; __builtin_memcpy(&u, &x, 4); return vt::scale_exponent(u); }
 }
 """
@@ -189,6 +189,7 @@ def cells(tmp_path_factory):
     L.page.argtypes, L.page.restype = [i32, i64, i32, i32, i32], i64
     L.tokens.argtypes = [i32, i64]
     L.rows.argtypes = [ctypes.c_void_p, i32, i64, i32, ctypes.POINTER(i64)]
+    L.share.argtypes = [i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
     L.exponent.argtypes = [ctypes.c_float]
     return L
 
@@ -224,13 +225,17 @@ def test_lengths_and_rows_stay_within_what_there_is(cells):
     assert got == [3, 0, 5, 0, 0, 0, 5, 0]
 
 
-def test_pieces_cover_every_token_once(cells):
-    for tokens in (0, 1, 127, 128, 129, 5000, 131072, (1 << 30) - 1, 1 << 30):
-        for splits in (1, 2, 7, 256):
-            piece = cells.piece(tokens, splits, 128)
-            pieces = cells.pieces(tokens, piece)
-            assert piece % 128 == 0 and 1 <= pieces <= splits
-            assert pieces * piece >= tokens and (pieces - 1) * piece < max(tokens, 1)
+def test_shares_cover_every_step_once(cells):
+    assert [cells.steps(t, 1, 128) for t in (0, 1, 128, 129, 256, 257, 1 << 30)] == [1, 1, 1, 2, 2, 3, 1 << 23] and cells.steps(500, 0, 128) == 0
+    per, start = ctypes.c_int32(), ctypes.c_int32()
+    for all_ in (0, 1, 5, 64, 65, 1000, (1 << 30) - 1, 1 << 30):
+        for places in (1, 2, 7, 64, 512):
+            upto = 0
+            for place in range(places):
+                left = cells.share(all_, places, place, ctypes.byref(per), ctypes.byref(start))
+                assert left >= 0 and (left == 0 or start.value == upto) and left <= per.value
+                upto += left
+            assert upto == all_
 
 
 def test_scales_are_the_smallest_that_hold_the_maximum(cells):
