@@ -13,6 +13,7 @@ import ctypes
 
 import torch
 
+from . import binding
 from .binding import VT_I32, VT_I64, _check, _dtype_code, _ptr, _require_cuda, _scratch, _stream, load_library
 
 VT_E4M3 = 2
@@ -34,6 +35,13 @@ def rope_table(positions: int, rotary_dim: int, base: float = 10000.0, device="c
 
 
 # --------------------------------------------------------------------------- arguments
+# The native way (csrc/vt_bind.cpp) checks, makes the results and calls; it answers None to a call that is not plain, which goes on below.
+def _got(got):
+    if type(got) is int:
+        _check(got)
+    return got
+
+
 def _heads(t: torch.Tensor, n: int, heads: int, D: int, dtype) -> int:
     """The row stride of a tensor of heads, checked."""
     if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or tuple(t.shape) != (n, heads, D):
@@ -99,6 +107,10 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
 
     `q_out` / `k_out` supply the results (q and k themselves, say).  Where a gradient is asked for, it comes from
     qk_norm_rope_backward."""
+    if binding._bind is not None:
+        got = binding._bind.norm(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
+        if got is not None:
+            return _got(got)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
         if q_out is not None or k_out is not None:
             raise ValueError("q_out and k_out are for calls without gradients")
@@ -128,6 +140,10 @@ def qk_norm_rope_backward(gq: torch.Tensor, gk: torch.Tensor, q: torch.Tensor, k
     """Gradients of qk_norm_rope from those of its results, (dq, dk, dq_weight, dk_weight): the weights' in float32 [D] (None
     without weights).  `dq` / `dk` supply the results (gq and gk themselves, say)."""
     L = load_library()
+    if binding._bind is not None and dq is None and dk is None and ws is None:
+        got = binding._bind.norm_backward(gq, gk, q, k, positions, table, q_weight, k_weight, eps, interleaved)
+        if got is not None:
+            return _got(got)
     n, hq, D = q.shape
     hk = k.shape[1]
     qs, ks = _heads(q, n, hq, D, q.dtype), _heads(k, n, hk, D, q.dtype)
@@ -215,6 +231,10 @@ def qkv_to_cache(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, cache
     """qk_norm_rope on q and k, with k and v written to the cache at `slots` (outside it: not written), in one launch.
     Returns q' (None without q)."""
     L = load_library()
+    if binding._bind is not None and q is not None and type(cache) is KVCache:
+        got = binding._bind.to_cache(q, k, v, cache._address, slots, positions, table, q_weight, k_weight, eps, interleaved, q_out)
+        if got is not None:
+            return _got(got)
     n, hk, D = k.shape
     if hk != cache.heads or D != cache.head_dim:
         raise ValueError("k and v must have the cache's heads")
@@ -243,6 +263,10 @@ def kv_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
                   v_out: torch.Tensor | None = None):
     """The cache's rows at `slots` as values, (k, v) [n, heads, head_dim]; zeros for slots outside it."""
     L = load_library()
+    if binding._bind is not None and k_out is None and v_out is None and type(cache) is KVCache and dtype in (torch.bfloat16, torch.float32):
+        got = binding._bind.cache_read(cache._address, slots, dtype == torch.float32)
+        if got is not None:
+            return _got(got)
     n = slots.numel()
     shape = (n, cache.heads, cache.head_dim)
     if k_out is None:
@@ -281,6 +305,11 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     the last 64 tokens a row sees, bit j being token length - 64 + j.  scale: of the scores (head_dim^-1/2).
     max_length: no request is longer (the page table's width, where it isn't given; near the longest is fastest)."""
     L = load_library()
+    if binding._bind is not None and type(ws) is AttentionWorkspace and type(cache) is KVCache:
+        got = binding._bind.attend(q, cache._address, page_table, lengths, row_start, max_rows, tail_mask, max_length, scale, ws.buf, out, return_lse,
+                                   out_lse)
+        if got is not None:
+            return _got(got)
     n, hq, D = q.shape
     _require_cuda(page_table, lengths, row_start, tail_mask, out_lse)
     if page_table.dtype != torch.int32 or page_table.dim() != 2 or lengths.dtype != torch.int32:

@@ -134,7 +134,9 @@ def _connect(L) -> None:
     if _raw_stream is None or getattr(_vt_bind, "built_for", None) != BIND_ABI:
         return
     _vt_bind.connect(_raw_stream, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        L.vt_draft_head_step, L.vt_draft_head_step_static, L.vt_draft_tree_level, L.vt_tree_rerank, L.vt_count_tokens)))
+        L.vt_draft_head_step, L.vt_draft_head_step_static, L.vt_draft_tree_level, L.vt_tree_rerank, L.vt_count_tokens,
+        L.vt_qk_norm_rope, L.vt_qk_norm_rope_backward, L.vt_qk_norm_rope_backward_ws_bytes, L.vt_qkv_to_cache, L.vt_kv_cache_read,
+        L.vt_paged_attention)))
     _bind = _vt_bind
 
 

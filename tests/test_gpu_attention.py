@@ -4,12 +4,14 @@ Tolerances count roundings: half a step of a type is finfo.eps / 2 relative.  fp
 test); a result in bf16 adds its one rounding.  Attention of bf16 rows rounds its weights p once to bf16 as well, which are at most all
 2^-9 off in the same direction.
 """
+import ctypes
 import math
 
 import pytest
 import torch
 
 import paper_2506_22694_amd as vt
+from paper_2506_22694_amd import binding
 
 pytestmark = pytest.mark.gpu
 
@@ -687,3 +689,89 @@ def test_refusals_on_the_device():
         with pytest.raises(vt.VocabTrimError) as e:
             call()
         assert e.value.status == status
+
+
+# ---------------------------------------------------------------------------------------------- the native way through the binding
+def _layer_calls():
+    """name -> (call, arguments) of the attention's calls, plain ones."""
+    g = _gen(20)
+    n, hq, hk, D, page = 5, 4, 2, 64, 16
+    q, k, v = (_randn(g, n, h, D).to(BF16) for h in (hq, hk, hk))
+    w = torch.ones(D, device="cuda", dtype=BF16)
+    rope, positions = _table64(40, 32), torch.arange(n, device="cuda")
+    cache, table, lengths, rows, starts = _case(g, E4M3, BF16, hq, hk, D, page, [400, 30], rows=[3, 2])
+    ws = vt.AttentionWorkspace(n, hq, hk, D, 2, 3, 512, "cuda")
+    norm = dict(positions=positions, table=rope, q_weight=w, k_weight=w, eps=1e-5, interleaved=True)
+    mask = torch.randint(-(1 << 62), 1 << 62, (n,), generator=g, device="cuda")
+    return {
+        "norm": (vt.qk_norm_rope, dict(q=q, k=k, **norm, q_out=torch.empty_like(q))),
+        "norm alone": (vt.qk_norm_rope, dict(q=q, k=k, q_weight=w, k_weight=w)),
+        "backward": (vt.qk_norm_rope_backward, dict(gq=q + 1, gk=k + 1, q=q, k=k, **norm)),
+        "to cache": (vt.qkv_to_cache, dict(q=q, k=k, v=v, cache=cache, slots=torch.arange(n, device="cuda", dtype=torch.int32), **norm)),
+        "read": (vt.kv_cache_read, dict(cache=cache, slots=torch.arange(9, device="cuda"))),
+        "attend": (vt.paged_attention, dict(q=rows, cache=cache, page_table=table, lengths=lengths, row_start=starts, max_rows=3, tail_mask=mask,
+                                            max_length=512, scale=0.2, ws=ws, return_lse=True)),
+        "attend rows": (vt.paged_attention, dict(q=rows[:2], cache=cache, page_table=table, lengths=lengths, ws=ws, out_lse=torch.empty(2, hq, device="cuda"))),
+    }
+
+
+def _outcome(call, args):
+    try:
+        got = call(**args)
+    except (RuntimeError, ValueError, TypeError, AttributeError, IndexError, OverflowError, ctypes.ArgumentError) as e:
+        return type(e).__name__ if not isinstance(e, vt.VocabTrimError) else e.status
+    torch.cuda.synchronize()
+    return [x.clone() for x in (got if isinstance(got, tuple) else (got,)) if x is not None]      # (no q, no result; no weights, no gradients of them)
+
+
+def test_the_native_way_and_pythons_give_the_same(monkeypatch):
+    vt.load_library()
+    native = binding._bind
+    assert native is not None
+    for name, (call, args) in _layer_calls().items():
+        cases = [("plain", args)]
+        for key, t in args.items():
+            if isinstance(t, torch.Tensor):
+                cases += [(key + " on the host", {**args, key: t.cpu()}), (key + " of another type", {**args, key: t.to(torch.float64)}),
+                          (key + " no tensor", {**args, key: 3}), (key + " left out", {**args, key: None}), (key + " shorter", {**args, key: t[:-1].contiguous()})]
+                if t.dim() == 3:
+                    apart = torch.empty(t.shape[0], t.shape[1] + 2, t.shape[2], dtype=t.dtype, device="cuda")[:, 1:-1]
+                    apart.copy_(t)
+                    cases += [(key + " with rows apart", {**args, key: apart}), (key + " strided", {**args, key: t.repeat_interleave(2, -1)[..., ::2]}),
+                              (key + " without rows", {**args, key: t[:0]}), (key + " transposed", {**args, key: t.transpose(0, 1)})]
+            elif isinstance(t, (int, float)) and not isinstance(t, bool):
+                cases += [(f"{key} = {v}", {**args, key: v}) for v in (0, -1, 1 << 40, 2.5, math.nan, "1")]
+        for what, changed in cases:
+            both = []
+            for way in (native, None):
+                monkeypatch.setattr(binding, "_bind", way)
+                both.append(_outcome(call, changed))
+            assert type(both[0]) is type(both[1]), (name, what, both)
+            if isinstance(both[0], list):
+                for x, y in zip(*both):
+                    assert x.dtype == y.dtype and x.shape == y.shape and torch.equal(x.nan_to_num(9.0), y.nan_to_num(9.0)), (name, what)
+            else:
+                assert both[0] == both[1], (name, what, both)
+            assert what != "plain" or isinstance(both[0], list), (name, both)
+
+
+def test_plain_calls_take_the_native_way(monkeypatch):
+    asked = []
+
+    class Spy:
+        def __getattr__(self, name):
+            def call(*a):
+                got = getattr(native, name)(*a)
+                asked.append((name, got is not None))
+                return got
+            return call
+    vt.load_library()
+    native = binding._bind
+    monkeypatch.setattr(binding, "_bind", Spy())
+    for name, (call, args) in _layer_calls().items():
+        call(**args)
+        assert asked[-1][1], name
+    q = torch.ones(2, 2, 64, device="cuda", requires_grad=True)
+    y, _ = vt.qk_norm_rope(q, q.detach(), None, None, torch.nn.Parameter(torch.ones(64, device="cuda")), torch.ones(64, device="cuda"))
+    assert asked[-1] == ("norm", False) and y.requires_grad
+    torch.cuda.synchronize()
