@@ -9,6 +9,7 @@ namespace vt {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kNormBackwardWorkgroups = 1024;      // four on each CU
 
 // The eight values of a lane: two runs of four.  Pairs (x[j], x[4 + j]) for halves, (x[2 j], x[2 j + 1]) for neighbours.
 struct Lane {
@@ -35,9 +36,24 @@ __device__ __forceinline__ void load8(const void *base, int64_t at, const Lane &
 template <typename T>
 __device__ __forceinline__ void store8(void *base, int64_t at, const Lane &l, const float *x) {
     typename T::store *p = static_cast<typename T::store *>(base) + at;
-    T::store4(p + l.o0, x);
-    T::store4(p + l.o1, x + 4);
+    T::stream4(p + l.o0, x);
+    T::stream4(p + l.o1, x + 4);
 }
+
+// The same as it is stored: rows that are asked for ahead of their use
+template <typename T>
+struct Raw8 {
+    typename T::raw4 a, b;
+    __device__ __forceinline__ void load(const void *base, int64_t at, const Lane &l) {
+        const typename T::store *p = static_cast<const typename T::store *>(base) + at;
+        a = *reinterpret_cast<const typename T::raw4 *>(p + l.o0);
+        b = *reinterpret_cast<const typename T::raw4 *>(p + l.o1);
+    }
+    __device__ __forceinline__ void open(float *x) const {
+        T::open4(a, x);
+        T::open4(b, x + 4);
+    }
+};
 
 struct Angle {
     float c[4], s[4];
@@ -103,8 +119,11 @@ __device__ __forceinline__ void to_cache(const CacheArgs &c, bool is_v, int64_t 
     if (l.pair == 0) (is_v ? c.v_scale : c.k_scale)[cell] = (uint8_t)e;
 }
 
+constexpr int kRowsAhead = 4;
+
 template <typename T, int GL>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
+    constexpr int GROUPS = kThreads / GL;
     const int group = threadIdx.x / GL;
     const Lane l = lane_of(threadIdx.x % GL, a);
     const int heads = a.hq + a.hk + (a.v != nullptr ? a.hk : 0);
@@ -115,29 +134,43 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
         load8<T>(a.wk, 0, l, wk);
     }
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const Angle t = angle_of(a, l, row);
-        const int64_t slot = a.to_cache ? index_at(a.slots, row) : 0;
-        for (int r = group; r < heads; r += kThreads / GL) {
-            const bool is_q = r < a.hq, is_v = r >= a.hq + a.hk;
-            const int head = is_q ? r : is_v ? r - a.hq - a.hk : r - a.hq;
-            float x[8] = {};
-            if (l.active)
-                load8<T>(is_q ? a.q : is_v ? a.v : a.k, row * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + head * a.D, l, x);
-            if (norm && !is_v) {
-                float ss = 0.0f;
+        for (int base = group; base < heads; base += kRowsAhead * GROUPS) {
+            // all of a group's rows of the token at a time: 16 bytes a lane would leave too little under way
+            Raw8<T> raw[kRowsAhead] = {};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss += x[j] * a.inverse_D * x[j];      // (a mean all along: squares that fit do not overflow as a sum)
-                const float rms = rsqrtf(group_sum<GL>(ss) + a.eps);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = x[j] * rms * (is_q ? wq[j] : wk[j]);
+            for (int u = 0; u < kRowsAhead; ++u) {
+                const int r = base + u * GROUPS;
+                if (r >= heads || !l.active) continue;
+                const bool is_q = r < a.hq, is_v = r >= a.hq + a.hk;
+                const int head = is_q ? r : is_v ? r - a.hq - a.hk : r - a.hq;
+                raw[u].load(is_q ? a.q : is_v ? a.v : a.k, row * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + head * a.D, l);
             }
-            if (!is_v && l.turns) turn<1>(x, t, a.neighbours);
-            if (is_q) {
-                if (l.active) store8<T>(a.q_out, row * a.q_out_stride + head * a.D, l, x);
-            } else if (!a.to_cache) {
-                if (l.active) store8<T>(a.k_out, row * a.k_out_stride + head * a.D, l, x);
-            } else {
-                to_cache<GL>(a.cache, is_v, row_of_slot(slot, a.cache.pages, a.cache.heads, head, a.cache.page_shift), l, x);
+            const Angle t = angle_of(a, l, row);
+            const int64_t slot = a.to_cache ? index_at(a.slots, row) : 0;
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u) {
+                const int r = base + u * GROUPS;
+                if (r >= heads) break;
+                const bool is_q = r < a.hq, is_v = r >= a.hq + a.hk;
+                const int head = is_q ? r : is_v ? r - a.hq - a.hk : r - a.hq;
+                float x[8];
+                raw[u].open(x);
+                if (norm && !is_v) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) ss += x[j] * a.inverse_D * x[j];      // (a mean all along: squares that fit do not overflow as a sum)
+                    const float rms = rsqrtf(group_sum<GL>(ss) + a.eps);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = x[j] * rms * (is_q ? wq[j] : wk[j]);
+                }
+                if (!is_v && l.turns) turn<1>(x, t, a.neighbours);
+                if (is_q) {
+                    if (l.active) store8<T>(a.q_out, row * a.q_out_stride + head * a.D, l, x);
+                } else if (!a.to_cache) {
+                    if (l.active) store8<T>(a.k_out, row * a.k_out_stride + head * a.D, l, x);
+                } else {
+                    to_cache<GL>(a.cache, is_v, row_of_slot(slot, a.cache.pages, a.cache.heads, head, a.cache.page_shift), l, x);
+                }
             }
         }
     }
@@ -147,8 +180,11 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
 // r is found again from x, which the sums need anyway.  A workgroup takes rows blockIdx.x, + gridDim.x, ... and keeps its sums for the
 // weights in registers, eight values a lane; the lanes of the same columns are added in LDS at its end, and the workgroups' sums in a
 // kernel of their own, both in a fixed order.
+constexpr int kBackwardAhead = 4;
+
 template <typename T, int GL>
 __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(NormArgs a) {
+    constexpr int GROUPS = kThreads / GL;
     __shared__ float sums[kThreads * 8];
     const int group = threadIdx.x / GL;
     const Lane l = lane_of(threadIdx.x % GL, a);
@@ -160,34 +196,49 @@ __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(NormArgs a
         load8<T>(a.wk, 0, l, wk);
     }
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const Angle t = angle_of(a, l, row);
-        for (int r = group; r < heads; r += kThreads / GL) {
-            const bool is_q = r < a.hq;
-            const int head = is_q ? r : r - a.hq;
-            float g[8] = {}, x[8] = {};
-            if (l.active) load8<T>(is_q ? a.gq : a.gk, row * (is_q ? a.gq_stride : a.gk_stride) + head * a.D, l, g);
-            if (norm && l.active) load8<T>(is_q ? a.q : a.k, row * (is_q ? a.q_stride : a.k_stride) + head * a.D, l, x);
-            if (l.turns) turn<-1>(g, t, a.neighbours);
-            if (norm) {
-                float ss = 0.0f;
+        for (int base = group; base < heads; base += kBackwardAhead * GROUPS) {
+            Raw8<T> rg[kBackwardAhead] = {}, rx[kBackwardAhead] = {};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) ss += x[j] * a.inverse_D * x[j];      // (a mean all along: squares that fit do not overflow as a sum)
-                const float rms = rsqrtf(group_sum<GL>(ss) + a.eps);
-                float dot = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] *= rms;
-                    const float p = g[j] * x[j];
-                    sq[j] += is_q ? p : 0.0f;
-                    sk[j] += is_q ? 0.0f : p;
-                    g[j] *= is_q ? wq[j] : wk[j];
-                    dot += l.active ? g[j] * x[j] : 0.0f;
-                }
-                dot = group_sum<GL>(dot) * a.inverse_D;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = rms * (g[j] - x[j] * dot);
+            for (int u = 0; u < kBackwardAhead; ++u) {
+                const int r = base + u * GROUPS;
+                if (r >= heads || !l.active) continue;
+                const bool is_q = r < a.hq;
+                const int head = is_q ? r : r - a.hq;
+                rg[u].load(is_q ? a.gq : a.gk, row * (is_q ? a.gq_stride : a.gk_stride) + head * a.D, l);
+                if (norm) rx[u].load(is_q ? a.q : a.k, row * (is_q ? a.q_stride : a.k_stride) + head * a.D, l);
             }
-            if (l.active) store8<T>(is_q ? a.q_out : a.k_out, row * (is_q ? a.q_out_stride : a.k_out_stride) + head * a.D, l, g);
+            const Angle t = angle_of(a, l, row);
+#pragma unroll
+            for (int u = 0; u < kBackwardAhead; ++u) {
+                const int r = base + u * GROUPS;
+                if (r >= heads) break;
+                const bool is_q = r < a.hq;
+                const int head = is_q ? r : r - a.hq;
+                float g[8], x[8];
+                rg[u].open(g);
+                rx[u].open(x);
+                if (l.turns) turn<-1>(g, t, a.neighbours);
+                if (norm) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) ss += x[j] * a.inverse_D * x[j];
+                    const float rms = rsqrtf(group_sum<GL>(ss) + a.eps);
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] *= rms;
+                        const float p = g[j] * x[j];
+                        sq[j] += is_q ? p : 0.0f;
+                        sk[j] += is_q ? 0.0f : p;
+                        g[j] *= is_q ? wq[j] : wk[j];
+                        dot += l.active ? g[j] * x[j] : 0.0f;
+                    }
+                    dot = group_sum<GL>(dot) * a.inverse_D;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] = rms * (g[j] - x[j] * dot);
+                }
+                if (l.active) store8<T>(is_q ? a.q_out : a.k_out, row * (is_q ? a.q_out_stride : a.k_out_stride) + head * a.D, l, g);
+            }
         }
     }
     if (!norm) return;
@@ -209,20 +260,31 @@ __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(NormArgs a
     }
 }
 
-// Columns of [workgroups, 2 * D] added up: 16 columns and 16 shares of the workgroups to a workgroup.
-__global__ __launch_bounds__(kThreads) void norm_weight_sums_kernel(NormArgs a, int workgroups) {
-    __shared__ float sums[16][17];
-    const int c = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
-    float s = 0.0f;
-    if (c < 2 * a.D) {
-        for (int i = part; i < workgroups; i += 16) s += a.partial[(int64_t)i * 2 * a.D + c];
+// Columns of [workgroups, 2 * D] added up: 8 columns and 128 shares of the workgroups to a workgroup, a share's rows all under way at a time
+// (1024 rows in 16 shares, a row after the other: 20.6 us).
+constexpr int kSumThreads = 1024, kSumColumns = 8;
+__global__ __launch_bounds__(kSumThreads) void norm_weight_sums_kernel(NormArgs a, int workgroups) {
+    constexpr int SHARES = kSumThreads / kSumColumns;
+    __shared__ float sums[SHARES][kSumColumns + 1];
+    const int column = threadIdx.x % kSumColumns, c = blockIdx.x * kSumColumns + column, share = threadIdx.x / kSumColumns;
+    float s = 0.0f;      // (2 * D is a multiple of 16: every column exists)
+    constexpr int PER = kNormBackwardWorkgroups / SHARES;
+    float x[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int w = share + i * SHARES;
+        x[i] = a.partial[(int64_t)min(w, workgroups - 1) * 2 * a.D + c];
+        x[i] = w < workgroups ? x[i] : 0.0f;
     }
-    sums[part][threadIdx.x % 16] = s;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s += x[i];
+    sums[share][column] = s;
     __syncthreads();
-    if (part != 0 || c >= 2 * a.D) return;
-    s = 0.0f;
-    for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x];
-    (c < a.D ? a.dqw : a.dkw - a.D)[c] = s;
+    for (int half = SHARES / 2; half > 0; half /= 2) {
+        if (share < half) sums[share][column] += sums[share + half][column];
+        __syncthreads();
+    }
+    if (share == 0) (c < a.D ? a.dqw : a.dkw - a.D)[c] = sums[0][column];
 }
 
 // Rows of the cache as values: GL lanes to a head row, eight values a lane.
@@ -256,8 +318,8 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a) {
                 }
             }
             typename T::store *p = static_cast<typename T::store *>(which ? a.v_out : a.k_out) + r * a.cache.D + o;
-            T::store4(p, x);
-            T::store4(p + 4, x + 4);
+            T::stream4(p, x);
+            T::stream4(p + 4, x + 4);
         }
     }
 }
@@ -290,7 +352,7 @@ void run_read(const CacheReadArgs &a, hipStream_t st) {
 
 }  // namespace
 
-int norm_backward_workgroups(int64_t n) { return n < 1024 ? (n < 1 ? 1 : (int)n) : 1024; }
+int norm_backward_workgroups(int64_t n) { return n < kNormBackwardWorkgroups ? (n < 1 ? 1 : (int)n) : kNormBackwardWorkgroups; }
 
 hipError_t launch_norm_rope(const NormArgs &args, bool bf16, hipStream_t st) {
     NormArgs a = args;
@@ -304,7 +366,7 @@ hipError_t launch_norm_rope_backward(const NormArgs &args, bool bf16, hipStream_
     bf16 ? run_backward<Bf16>(a, st) : run_backward<F32>(a, st);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.wq == nullptr) return e;
-    norm_weight_sums_kernel<<<(2 * a.D + 15) / 16, kThreads, 0, st>>>(a, norm_backward_workgroups(a.n));
+    norm_weight_sums_kernel<<<2 * a.D / kSumColumns, kSumThreads, 0, st>>>(a, norm_backward_workgroups(a.n));
     return hipGetLastError();
 }
 hipError_t launch_cache_read(const CacheReadArgs &a, bool bf16, hipStream_t st) {

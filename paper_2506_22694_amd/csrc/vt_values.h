@@ -17,22 +17,29 @@ __device__ __forceinline__ float high_bf16(unsigned u) { return __uint_as_float(
 
 struct Bf16 {
     typedef uint16_t store;
-    static __device__ __forceinline__ void load4(const store *p, float *x) {
-        const u32x2 u = *reinterpret_cast<const u32x2 *>(p);
+    typedef u32x2 raw4;      // four values as they are stored
+    static __device__ __forceinline__ void open4(raw4 u, float *x) {
         x[0] = low_bf16(u.x), x[1] = high_bf16(u.x), x[2] = low_bf16(u.y), x[3] = high_bf16(u.y);
     }
+    static __device__ __forceinline__ void load4(const store *p, float *x) { open4(*reinterpret_cast<const raw4 *>(p), x); }
     static __device__ __forceinline__ void store4(store *p, const float *x) {
         *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    }
+    // ... past the caches' order of use: what a kernel writes once and does not read
+    static __device__ __forceinline__ void stream4(store *p, const float *x) {
+        __builtin_nontemporal_store(u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])}, reinterpret_cast<u32x2 *>(p));
     }
 };
 struct F32 {
     typedef float store;
-    static __device__ __forceinline__ void load4(const store *p, float *x) {
-        const f32x4v u = *reinterpret_cast<const f32x4v *>(p);
-        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
-    }
+    typedef f32x4v raw4;
+    static __device__ __forceinline__ void open4(raw4 u, float *x) { x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w; }
+    static __device__ __forceinline__ void load4(const store *p, float *x) { open4(*reinterpret_cast<const raw4 *>(p), x); }
     static __device__ __forceinline__ void store4(store *p, const float *x) {
         *reinterpret_cast<f32x4v *>(p) = f32x4v{x[0], x[1], x[2], x[3]};
+    }
+    static __device__ __forceinline__ void stream4(store *p, const float *x) {
+        __builtin_nontemporal_store(f32x4v{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4v *>(p));
     }
 };
 
