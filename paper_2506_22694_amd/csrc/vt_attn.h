@@ -26,7 +26,9 @@ struct NormArgs {
     int64_t n;
     int hq, hk, D, rot, neighbours;
     const void *wq, *wk;        // null: no norm
-    float eps, inverse_D;       // (inverse_D: set by the launch)
+    float eps;
+    float inverse_D;            // (set by the launch, this and the next: 1 / D; tokens that a workgroup takes at a time)
+    int tokens_log2;
     const float *table;         // null: no rotation
     int64_t table_rows;
     IndexArgs positions;
