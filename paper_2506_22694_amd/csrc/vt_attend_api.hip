@@ -66,9 +66,10 @@ struct Split {
     size_t entries = 0, bytes = 0, most_bytes = 0;       // rows of partial results; bytes of this call; of any call of up to these sizes
 };
 
-// Shares that all requests' tokens are cut into: two workgroups' on each of the 256 CUs, all there at a time.  With half as many the ragged
-// 8-bit batch takes 107 us instead of 104 and 131001 tokens of one request 88.0 instead of 88.8; with twice as many 106 and 92.
-constexpr int64_t kAttendWorkgroups = 512;
+// Shares that all requests' tokens are cut into: two workgroups' on each of the 256 CUs, all there at a time, the one reading while the other
+// begins or ends a request (48 ragged requests in 8 bits 104 us, with one on each CU 107, with four 106).  One request has one beginning,
+// and the workgroups of a CU take each other's time: 16384 tokens 17.2 us with one on each CU, 18.5 with two; 131001 tokens 88.0 and 88.8.
+constexpr int64_t kAttendWorkgroups = 512, kAttendWorkgroupsOfOne = 256;
 // Up to here a workgroup takes a request whole, without the second launch: 300 tokens 6.6 us whole, 7.9 in shares; 512 tokens 8.9 and 8.0.
 constexpr int64_t kAttendWhole = 384;
 
@@ -86,7 +87,7 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     s.whole = max_length <= kAttendWhole;
     int64_t places = requests;
     if (!s.whole) {
-        places = (kAttendWorkgroups + units - 1) / units;
+        places = ((requests == 1 ? kAttendWorkgroupsOfOne : kAttendWorkgroups) + units - 1) / units;
         if (places > steps * requests) places = steps * requests;
     }
     if (places * units > kMaxGrid || places > 65535) return s;

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
     // another wave's loads fill the time.
     constexpr bool LEAN = DP > 128;
     __shared__ float2 ms[W][16 * NT];
-    __shared__ __align__(16) float sums[W][16][PITCH];
+    __shared__ __align__(16) float sums[W][16 * NT][PITCH];
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     // Workgroups go to the XCDs in turn: heads first, which have equal work, then the shares of a head's, which have too.
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     // (a row that has seen nothing yet: exp2(-inf - 0) = 0)
                     const float base = most == kNone ? 0.0f : most;
                     const float fade = __builtin_amdgcn_exp2f(top[nt] - base);
-                    if (__any(most > top[nt])) {
+                    if (token != t0 + kAttendTile * wave && __any(most > top[nt])) {      // (the first tile has nothing to rescale)
 #pragma unroll
                         for (int i = 0; i < E; ++i) {
 #pragma unroll
@@ -559,15 +559,21 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
             for (int w = 0; w < W; ++w) all += part[w].y == 0.0f ? 0.0f : part[w].y * __builtin_amdgcn_exp2f(part[w].x - most);
             float fade = total[nt] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(top[nt] - most);
             if (complete) fade = all == 0.0f ? 0.0f : fade / all;
-            if (nt != 0) __syncthreads();
+            if (__any(total[nt] == 0.0f)) {      // (values of infinity times p = 0 may be there)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[nt][i][r] = total[nt] == 0.0f ? 0.0f : acc[nt][i][r];
+                }
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
 #pragma unroll
                 for (int i = 0; i < E; i += 4) {
                     float o[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = total[nt] == 0.0f ? 0.0f : acc[nt][i + j][r] * fade;
-                    F32::store4(&sums[wave][m][4 * E * g + E * r + i], o);
+                    for (int j = 0; j < 4; ++j) o[j] = acc[nt][i + j][r] * fade;
+                    F32::store4(&sums[wave][16 * nt + m][4 * E * g + E * r + i], o);
                 }
             }
             if (wave == 0 && g == 0 && 16 * nt + m < RG) {
@@ -575,28 +581,28 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                 if (!complete) a.part_ms[kept_at * (16 * NT) + 16 * nt + m] = make_float2(most, all);
                 else if (a.lse != nullptr) a.lse[(first + x0_row + up) * a.hq + h * a.G + y - up * a.G] = log_sum_exp(most, all);
             }
-            __syncthreads();
-            constexpr int PER = 64 * W / (DP / 4);      // rows that the workgroup takes at a time
-            const int d = 4 * (thread % (DP / 4));
+        }
+        __syncthreads();
+        constexpr int PER = 64 * W / (DP / 4);      // rows that the workgroup takes at a time
+        const int d = 4 * (thread % (DP / 4));
 #pragma unroll
-            for (int c = 0; c < 16; c += PER) {
-                const int xr = c + thread / (DP / 4), x = 16 * nt + xr;
-                if (x >= RG || d >= D) continue;
-                float o[4] = {};
+        for (int c = 0; c < 16 * NT; c += PER) {
+            const int x = c + thread / (DP / 4);
+            if (x >= RG || d >= D) continue;
+            float o[4] = {};
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    float u[4];
-                    F32::load4(&sums[w][xr][d], u);
+            for (int w = 0; w < W; ++w) {
+                float u[4];
+                F32::load4(&sums[w][x][d], u);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] += u[i];
-                }
-                if (!complete) {
-                    F32::store4(a.part_o + (kept_at * (16 * NT) + x) * D + d, o);
-                    continue;
-                }
-                const int y = x0_head + x, up = by_group(a, y);
-                store_values(a, (first + x0_row + up) * a.out_stride + (h * a.G + y - up * a.G) * D + d, o, F32Q);
+                for (int i = 0; i < 4; ++i) o[i] += u[i];
             }
+            if (!complete) {
+                F32::store4(a.part_o + (kept_at * (16 * NT) + x) * D + d, o);
+                continue;
+            }
+            const int y = x0_head + x, up = by_group(a, y);
+            store_values(a, (first + x0_row + up) * a.out_stride + (h * a.G + y - up * a.G) * D + d, o, F32Q);
         }
         if (share.left > 0) __syncthreads();
     }
