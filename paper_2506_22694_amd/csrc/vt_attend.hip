@@ -20,7 +20,9 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
         r = b % a.max_rows;
         b /= a.max_rows;
     }
+    // (every place has said what it begins; a request only if it has rows: nothing of one without is looked at)
     const int4 parts = a.part_at[b];
+    if (a.by_place) b = parts.w;
     int64_t first;
     if (r >= rows_of(a.row_start, b, a.n, a.max_rows, first) || parts.y == 1) return;
     const int h = head / a.G, rows = 16 * a.row_tiles, x = r * a.G + head - h * a.G, rb = x / rows;
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
 
 template <int LV>
 void run_join(const AttendArgs &a, bool f32, hipStream_t st) {
-    const dim3 grid((unsigned)(a.requests * a.max_rows), (unsigned)a.hq);
+    const dim3 grid((unsigned)((a.by_place ? a.places : a.requests) * a.max_rows), (unsigned)a.hq);
     if (f32) attend_join_kernel<LV, true><<<grid, kJoinThreads, 0, st>>>(a);
     else attend_join_kernel<LV, false><<<grid, kJoinThreads, 0, st>>>(a);
 }

@@ -70,8 +70,11 @@ struct Split {
 // begins or ends a request (48 ragged requests in 8 bits 104 us, with one on each CU 107, with four 106).  One request has one beginning,
 // and the workgroups of a CU take each other's time: 16384 tokens 17.2 us with one on each CU, 18.5 with two; 131001 tokens 88.0 and 88.8.
 constexpr int64_t kAttendWorkgroups = 512, kAttendWorkgroupsOfOne = 256;
-// Up to here a workgroup takes a request whole, without the second launch: 300 tokens 6.6 us whole, 7.9 in shares; 512 tokens 8.9 and 8.0.
-constexpr int64_t kAttendWhole = 384;
+// Up to here a workgroup takes a request whole, without the second launch: 300 tokens of one request 6.6 us whole, 7.9 in shares, 512 tokens
+// 8.9 and 8.0.  Where there are many requests the workgroups are enough: of two requests' worth of tokens for each workgroup and no more
+// than kAttendWholeOfMany (8-bit cache, 64 requests of up to 1000 tokens, 512 workgroups: 19.5 us whole, 26.0 in shares; 16 requests, 128
+// workgroups: 13.2 and 11.2; 64 requests of up to 4000: 60.5 and 46.0).
+constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32) {
     Split s;
@@ -84,7 +87,8 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     if (rows > kMaxGrid || (int64_t)requests * max_rows * q_heads > kMaxGrid || (steps + 1) * requests > kMaxLength) return s;
     s.row_tiles = vt::attend_row_tiles((int)rows, D, f32);
     const int64_t per = 16 * s.row_tiles, blocks = (rows + per - 1) / per, units = kv_heads * blocks;
-    s.whole = max_length <= kAttendWhole;
+    const int64_t few = 2 * units * requests < kAttendWholeOfMany ? 2 * units * requests : kAttendWholeOfMany;
+    s.whole = max_length <= (few > kAttendWhole ? few : kAttendWhole);
     int64_t places = requests;
     if (!s.whole) {
         places = ((requests == 1 ? kAttendWorkgroupsOfOne : kAttendWorkgroups) + units - 1) / units;
@@ -248,6 +252,7 @@ int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int
     a.out = out, a.out_stride = out_stride, a.lse = out_lse;
     a.whole = split.whole, a.places = split.places, a.row_blocks = split.row_blocks, a.row_tiles = split.row_tiles;
     a.G_magic = (unsigned)(((uint64_t)1 << 32) / a.G) + 1u;
+    a.by_place = n_requests > split.places;
     a.part_o = static_cast<float *>(ws);
     a.part_ms = reinterpret_cast<float2 *>(a.part_o + split.entries * cache->head_dim);
     a.part_at = reinterpret_cast<int4 *>(a.part_ms + split.entries);

@@ -171,6 +171,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         share.left = request_steps(share.r);
     } else {
         share = share_of(a, place);
+        if (share.left == 0 && a.by_place && blockIdx.x == 0 && threadIdx.x == 0) a.part_at[place] = make_int4(place, 1, 0, 0);
     }
 
     // A part of a request after another, most often one or two
@@ -191,8 +192,13 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
             else share.r = request_of(a, ++share.b);
             share.at = 0;
         }
-        if (!a.whole && take > 0 && at_step == 0 && blockIdx.x == 0 && thread == 0)
-            a.part_at[b] = make_int4(place, complete ? 1 : 1 + (steps - take + share.per - 1) / share.per, segment != 0, 0);
+        // For the join: where the parts of each request are, or of the one request that a place may begin and not end.
+        if (!a.whole && blockIdx.x == 0 && thread == 0) {
+            const int4 parts = make_int4(place, complete ? 1 : 1 + (steps - take + share.per - 1) / share.per, segment != 0, b);
+            const bool begins = take > 0 && at_step == 0;
+            if (a.by_place) a.part_at[place] = begins ? parts : make_int4(place, 1, 0, b);
+            else if (begins) a.part_at[b] = parts;
+        }
         const int RG = nrows * a.G - x0;      // query rows from x0 on
         if (RG <= 0 || take <= 0) continue;
         const int t0 = at_step * kAttendLeast, t1 = complete ? len : min(len, t0 + take * kAttendLeast);

@@ -74,7 +74,8 @@ struct AttendArgs {
     unsigned G_magic;               // floor(2^32 / G) + 1, G > 1
     float *part_o;                  // [row_blocks, heads, places, 2, 16 row_tiles, D], the same of (max, sum),
     float2 *part_ms;
-    int4 *part_at;                  // [requests]: first place of a request's parts, how many, the first one's number there
+    int by_place;                   // requests are more than places
+    int4 *part_at;                  // [requests or places]: first place of a request's parts, how many, the first one's number there, request
 };
 // 16-row tiles of queries that one workgroup takes
 int attend_row_tiles(int rows, int D, bool f32);

@@ -238,6 +238,69 @@ def test_shares_cover_every_step_once(cells):
             assert upto == all_
 
 
+def _shared_out(cells, tokens, rows, places, step):
+    """What the workgroups of one kv head do with requests of `tokens` cached tokens and `rows` new rows, in the kernel's order: parts written
+    {(place, number there): (request, first step, steps)}, where the join is told to look {request: (place, parts, number)}, by place too."""
+    steps = [cells.steps(t, r, step) for t, r in zip(tokens, rows)]
+    written, by_request, by_place = {}, {}, {}
+    whole = []
+    per, start = ctypes.c_int32(), ctypes.c_int32()
+    for place in range(places):
+        left = cells.share(sum(steps), places, place, ctypes.byref(per), ctypes.byref(start))
+        if left == 0:
+            by_place[place] = (place, 1, 0, 0)
+            continue
+        b, before = 0, 0
+        while start.value >= before + steps[b]:
+            before += steps[b]
+            b += 1
+        at, segment = start.value - before, 0
+        while left > 0:
+            take = min(left, steps[b] - at)
+            complete = take == steps[b]
+            left -= take
+            parts = (place, 1 if complete else 1 + -(-(steps[b] - take) // per.value), int(segment != 0), b)
+            begins = take > 0 and at == 0
+            by_place[place] = parts if begins else (place, 1, 0, b)
+            if begins:
+                by_request[b] = parts
+            if take > 0 and complete:
+                whole.append(b)
+            elif take > 0:
+                assert (place, int(segment != 0)) not in written
+                written[place, int(segment != 0)] = (b, at, take)
+            b, at, segment = b + 1, 0, segment + 1
+    return steps, written, by_request, by_place, whole
+
+
+def test_the_join_finds_every_part_of_every_request(cells):
+    import random
+    rng = random.Random(7)
+    for _ in range(400):
+        n = rng.choice([1, 2, 5, 30, 200])
+        tokens = [rng.choice([0, 1, 128, rng.randint(0, 3000), rng.randint(0, 300)]) for _ in range(n)]
+        rows = [rng.choice([0, 1, 1, 4]) for _ in range(n)]
+        places = rng.choice([1, 2, 7, 64, 256])
+        steps, written, by_request, by_place, whole = _shared_out(cells, tokens, rows, places, 128)
+        assert set(by_place) == set(range(places))
+        assert set(by_request) == {b for b in range(n) if rows[b] > 0}
+        begun = {p[3]: p for p in by_place.values() if p[1] > 1}
+        for b in range(n):
+            if rows[b] == 0:
+                assert b not in begun and b not in whole
+                continue
+            place, parts, number, _ = by_request[b]
+            assert (parts == 1) == (b in whole) and (parts == 1 or begun[b] == by_request[b]) and (parts > 1 or b not in begun)
+            if parts > 1:
+                at = 0
+                for i in range(parts):
+                    of, first, took = written.pop((place + i, number if i == 0 else 0))
+                    assert of == b and first == at
+                    at += took
+                assert at == steps[b]
+        assert not written
+
+
 def test_scales_are_the_smallest_that_hold_the_maximum(cells):
     import random
     rng = random.Random(1)

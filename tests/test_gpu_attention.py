@@ -423,6 +423,18 @@ def test_attention_of_tree_levels(hq, hk, D, rows, held, dtype, masked):
         _check_attention(*case, mask=mask)
 
 
+@pytest.mark.parametrize("held", [BF16, E4M3])
+@pytest.mark.parametrize("rows", [None, 3])
+def test_attention_of_more_requests_than_shares(held, rows):
+    """Requests begin and end anywhere in the shares; some have no rows, some no tokens."""
+    g = _gen(30)
+    n = 90
+    lengths = [[1490, 0, 130, 128, 1, 700, 90, 260, 64][i * 7 % 9] for i in range(n)]
+    counts = None if rows is None else [i * 5 % (rows + 1) for i in range(n)]
+    case = _case(g, held, BF16, 8, 8, 64, 16, lengths, rows=counts)
+    _check_attention(*case, max_length=1504)
+
+
 def test_attention_single_rows_with_a_mask():
     g = _gen(3)
     case = _case(g, BF16, BF16, 8, 2, 64, 16, [70, 5, 0, 64, 2000])
