@@ -311,3 +311,16 @@ def test_scales_are_the_smallest_that_hold_the_maximum(cells):
         e = cells.exponent(x)
         assert 1 <= e <= 254 and x <= 448 * 2.0 ** (e - 127)
         assert e == 1 or x > 448 * 2.0 ** (e - 128)
+
+
+def test_build_rejects_attention_kernels_with_accumulation_registers():
+    from paper_2506_22694_amd import build
+    remarks = "\n".join([
+        "a.h:1:1: remark: Function Name: kernel_a [-Rpass-analysis=kernel-resource-usage]",
+        "a.h:1:1: remark:     VGPRs: 200 [-Rpass-analysis=kernel-resource-usage]",
+        "a.h:1:1: remark:     AGPRs: 0 [-Rpass-analysis=kernel-resource-usage]",
+        "a.h:1:1: remark: Function Name: kernel_b [-Rpass-analysis=kernel-resource-usage]",
+        "a.h:1:1: remark:     AGPRs: 12 [-Rpass-analysis=kernel-resource-usage]",
+    ])
+    assert build._accumulation_users(remarks) == [("kernel_b", 12)]
+    assert all(os.path.basename(s).startswith(build.NO_ACCUMULATION) for s in build._sources() if "vt_attend_d" in s)
