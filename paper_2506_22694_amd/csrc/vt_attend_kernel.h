@@ -47,6 +47,11 @@ __device__ __forceinline__ float row_sum(float v) {
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Sum over lanes l and l ^ 32
+__device__ __forceinline__ float half_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 // What is left of a value after its leading 8 bits
 __device__ __forceinline__ float less_bf16(float x, float &leading) {
     leading = (float)(__bf16)x;
