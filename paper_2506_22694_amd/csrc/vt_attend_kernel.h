@@ -123,7 +123,11 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     s.left = share_steps(all, a.places, place, s.per, start);
     if (s.left == 0) return s;
     int before = 0, base = 0;
-    while (start >= before + __builtin_amdgcn_readlane(upto, 63)) {      // (start is below the steps of all)
+    while (start >= before + __builtin_amdgcn_readlane(upto, 63)) {
+        if (base + 64 >= a.requests) {      // (start is below the steps of all, unless lengths are written to meanwhile)
+            s.left = 0;
+            return s;
+        }
         before += __builtin_amdgcn_readlane(upto, 63);
         base += 64;
         r = request(base + lane);
