@@ -102,8 +102,8 @@ typedef struct {
  *   q        NULL with q_heads == 0 writes the cache only
  *   k, v     [n, cache->heads, cache->head_dim]
  *   slots    [n] int32 or int64 (slot_type): where each row's k and v go.  A slot
- *            outside the cache (-1, say) leaves its row out.  Slots that occur
- *            twice have one of their rows' k and one of their rows' v. */
+ *            outside the cache (-1, say) leaves its row out.  A slot that
+ *            occurs twice holds no more than a mixture of its rows. */
 int vt_qkv_to_cache(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                     int type, int64_t n, int32_t q_heads, const void *q_weight, const void *k_weight, float eps,
                     const float *table, int64_t table_rows, int32_t rotary_dim, int style, const void *positions,
@@ -133,7 +133,8 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *   lengths      [n_requests] int32, n_requests <= VT_MAX_REQUESTS; below 0 counts as 0, above
  *                min(max_length, table_pages * page_size) as that
  *   row_start    [n_requests + 1] int32: rows row_start[b] .. row_start[b + 1] - 1 are
- *                request b's, at most max_rows of them (more are not computed);
+ *                request b's, at most max_rows of them (more, and rows of no
+ *                request, are not computed: their out and lse stay as they are);
  *                NULL: row i is the one row of request i, n == n_requests, max_rows == 1
  *   tail_mask    [n] uint64, nullable: bit j says whether the row sees token
  *                lengths[b] - 64 + j; tokens before those are seen by all rows

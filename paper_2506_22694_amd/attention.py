@@ -301,7 +301,7 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     """Attention of q [n, q_heads, head_dim] over the cached tokens of their requests: out like q [, lse float32 [n, q_heads]].
 
     page_table int32 [requests, pages of each], lengths int32 [requests].  Row i is request i's, or rows
-    row_start[b] .. row_start[b + 1] - 1 are request b's, at most max_rows.  tail_mask (int64 [n], its bits): which of
+    row_start[b] .. row_start[b + 1] - 1 are request b's, at most max_rows (other rows are not computed).  tail_mask (int64 [n], its bits): which of
     the last 64 tokens a row sees, bit j being token length - 64 + j.  scale: of the scores (head_dim^-1/2).
     max_length: no request is longer (the page table's width, where it isn't given; near the longest is fastest)."""
     L = load_library()

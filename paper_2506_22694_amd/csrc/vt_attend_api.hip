@@ -98,14 +98,14 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     s.ok = true;
     s.row_blocks = (int)blocks;
     s.places = (int)places;
-    if (s.whole) return s;
     const size_t entry = (D + 2) * sizeof(float);
+    // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
+    // larger with fewer rows.  (Fewer requests of the same lengths may be taken in shares where these are taken whole.)
+    const size_t most = 2 * (size_t)(kAttendWorkgroups * per + kv_heads * (rows + per));
+    s.most_bytes = max_length <= kAttendWhole ? 0 : round_up(most * entry + requests * sizeof(int4), 256);
+    if (s.whole) return s;
     s.entries = (size_t)units * places * 2 * per;
     s.bytes = s.entries * entry + requests * sizeof(int4);
-    // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
-    // larger with fewer rows.
-    const size_t most = 2 * (size_t)(kAttendWorkgroups * per + kv_heads * (rows + per));
-    s.most_bytes = round_up(most * entry + requests * sizeof(int4), 256);
     return s;
 }
 

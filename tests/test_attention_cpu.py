@@ -128,10 +128,10 @@ def test_workspace_for_the_largest_call_serves_all_below(lib):
     assert size(1, 32, 8, 128, 1, 1, 128) == 0 == size(9, 32, 8, 128, 70000, 1, 1 << 20) and size(1, 32, 7, 128, 1, 1, 1 << 20) == 0 and size(3, 32, 8, 128, 2, 1, 1 << 20) == 0
     import random
     rng = random.Random(3)
-    for _ in range(300):
+    for _ in range(3000):
         hk = rng.choice([1, 2, 8])
         hq, D = hk * rng.choice([1, 3, 4, 8]), rng.choice([64, 80, 128, 256])
-        requests, rows, most = rng.randint(1, 80), rng.randint(1, 20), rng.randint(0, 200000)
+        requests, rows, most = rng.randint(1, 80), rng.randint(1, 20), rng.choice([rng.randint(0, 2000), rng.randint(0, 200000)])
         whole = size(requests * rows, hq, hk, D, requests, rows, most)
         r, m, t = rng.randint(1, requests), rng.randint(1, rows), rng.randint(0, most)
         n = rng.randint(1, r * m)
