@@ -116,22 +116,31 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     const int lane = lane_id();
     auto request = [&](int i) { return i < a.requests ? request_of(a, i) : Request{0, 0, 0}; };
     Request r = request(lane);
-    int upto = wave_scan(request_steps(r)), all = __builtin_amdgcn_readlane(upto, 63);
-    for (int base = 64; base < a.requests; base += 64) all += __builtin_amdgcn_readlane(wave_scan(request_steps(request(base + lane))), 63);
+    const int mine = request_steps(r);
+    int sum = mine;
+#pragma unroll 4
+    for (int base = 64; base < a.requests; base += 64) sum += request_steps(request(base + lane));
+    const int all = a.requests <= 64 ? 0 : wave_sum_i32(sum);
+    int upto = wave_scan(mine), last = __builtin_amdgcn_readlane(upto, 63);
     Share s;
     int start;
-    s.left = share_steps(all, a.places, place, s.per, start);
+    s.left = share_steps(a.requests <= 64 ? last : __builtin_amdgcn_readfirstlane(all), a.places, place, s.per, start);
     if (s.left == 0) return s;
     int before = 0, base = 0;
-    while (start >= before + __builtin_amdgcn_readlane(upto, 63)) {
-        if (base + 64 >= a.requests) {      // (start is below the steps of all, unless lengths are written to meanwhile)
-            s.left = 0;
-            return s;
-        }
-        before += __builtin_amdgcn_readlane(upto, 63);
-        base += 64;
-        r = request(base + lane);
-        upto = wave_scan(request_steps(r));
+    if (start >= last) {
+        Request next = request(64 + lane);
+        do {
+            base += 64;
+            if (base >= a.requests) {      // (start is below the steps of all, unless lengths are written to meanwhile)
+                s.left = 0;
+                return s;
+            }
+            before += last;
+            r = next;
+            next = request(base + 64 + lane);      // (under way while this block is looked at)
+            upto = wave_scan(request_steps(r));
+            last = __builtin_amdgcn_readlane(upto, 63);
+        } while (start >= before + last);
     }
     const int at = __builtin_ctzll(__ballot(before + upto > start));
     s.b = base + at;

@@ -435,6 +435,17 @@ def test_attention_of_more_requests_than_shares(held, rows):
     _check_attention(*case, max_length=1504)
 
 
+def test_attention_of_hundreds_of_requests():
+    """Shares that begin in any block of 64 requests, whole blocks without rows."""
+    g = _gen(31)
+    n = 333
+    lengths = [(i * 37) % 400 if i % 11 else 0 for i in range(n)]
+    lengths[200] = 2000
+    counts = [0 if 64 <= i < 192 or i % 7 == 3 else 1 for i in range(n)]
+    case = _case(g, BF16, BF16, 2, 1, 64, 16, lengths, rows=counts)
+    _check_attention(*case, max_length=2048)
+
+
 def test_attention_single_rows_with_a_mask():
     g = _gen(3)
     case = _case(g, BF16, BF16, 8, 2, 64, 16, [70, 5, 0, 64, 2000])
