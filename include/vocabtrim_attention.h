@@ -143,8 +143,9 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *   out_lse      [n, q_heads] fp32, nullable
  *   ws           >= vt_paged_attention_ws_bytes(...) bytes, no initialisation; may be
  *                NULL where that is 0.  One for the largest batch serves smaller ones.
- * max_length and max_rows decide how the work is split: near the largest that occur
- * is fastest.  Only kernels are enqueued: the call may be captured in a graph.
+ * n_requests, max_rows and max_length decide how the work is cut up (many requests of
+ * few tokens are taken whole, a workgroup each, others in even shares of their
+ * lengths): near the largest that occur is fastest.  Only kernels are enqueued: the call may be captured in a graph.
  * ---------------------------------------------------------------------- */
 int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache,
                        const int32_t *page_table, int32_t table_pages, const int32_t *lengths, int32_t n_requests,

@@ -1,4 +1,4 @@
-// Attention over the cache: which kernel a shape gets, and the join of the pieces of long requests.
+// Attention over the cache: which kernel a shape gets, and the join of what several workgroups have of a request.
 #include "vt_attend_kernel.h"
 
 namespace vt {

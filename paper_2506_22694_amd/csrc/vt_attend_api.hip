@@ -1,4 +1,4 @@
-// C ABI of include/vocabtrim_attention.h: argument checks, how the work is split, kernel dispatch.  Every entry point only enqueues
+// C ABI of include/vocabtrim_attention.h: argument checks, how the work is cut up, kernel dispatch.  Every entry point only enqueues
 // work on the caller's stream.
 #include "vocabtrim_attention.h"
 
@@ -82,7 +82,7 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
         requests < 0 || requests > VT_MAX_REQUESTS || max_rows < 1 || n > (int64_t)requests * max_rows || max_length < 0 || max_length > kMaxLength)
         return s;
     const int64_t rows = (int64_t)max_rows * (q_heads / kv_heads);
-    const int64_t steps = (max_length + vt::kAttendLeast - 1) / vt::kAttendLeast;
+    const int64_t steps = (max_length + vt::kAttendStep - 1) / vt::kAttendStep;
     // (workgroups and threads of a launch, and all requests' steps, are 32-bit numbers)
     if (rows > kMaxGrid || (int64_t)requests * max_rows * q_heads > kMaxGrid || (steps + 1) * requests > kMaxLength) return s;
     s.row_tiles = vt::attend_row_tiles((int)rows, D, f32);

@@ -3,7 +3,7 @@
 // Bound by the one pass over the cached keys and values: a kv head's query rows (the heads that share it, times the request's new
 // tokens) are one side of the products, and up to 64 of them cost the matrix cores a fraction of the time that the cache takes to
 // arrive.  So what matters is that loads never stop, and a wave goes its own way: it takes 32 tokens at a time, straight from the cache
-// into registers in the matrix instructions' operand layout, without LDS and without a barrier until its piece of the request is done.
+// into registers in the matrix instructions' operand layout, without LDS and without a barrier until its part of the request is done.
 //
 //   scores^T [token, row] = K q^T      K's operand: lane l holds values of token l % 16, which are 16 bytes side by side in memory
 //   out^T [d, row] = V^T p^T           p's operand: lane l holds row l % 16 and 8 tokens -- those whose scores it has: what the
@@ -17,7 +17,12 @@
 // 8-bit caches: codes become bf16 (exactly) on their way, two for each conversion; scales are powers of two and go on the scores
 // and on p, where they are exact as well.
 //
-// fp32 rows: a value of 24 bits is the sum of three of 8, so q and p are three operands each, and products are exact as for bf16.
+// fp32 rows: a value of 24 bits is the sum of three of 8, so q and p are three operands each, and products are exact as for bf16.  bf16
+// rows have p rounded to bf16 once, after their sum was taken: with two operands for it results are off by 0.0017 instead of 0.0020 of
+// their size (0.0017 is their own rounding), and take up to 2.5 % longer.
+//
+// 131001 tokens of one request, 8 kv heads of 128 values in bf16, 4 query heads each: 537 MB in 80 us, 6.7 TB/s, where a plain read of as much
+// takes 79; 151 vector and 16 matrix instructions a tile (8 bits: 268 and 16; 48 ragged requests 541 MB in 94 us, 5.8 TB/s).
 #pragma once
 #include "vt_values.h"
 
@@ -104,7 +109,7 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, int b) {
     const int rows = rows_of(a.row_start, b, a.n, a.max_rows, first);
     return {tokens_of(a.lengths[b], a.most), rows, (int)first};
 }
-__device__ __forceinline__ int request_steps(const Request &r) { return steps_of(r.tokens, r.rows, kAttendLeast); }
+__device__ __forceinline__ int request_steps(const Request &r) { return steps_of(r.tokens, r.rows, kAttendStep); }
 
 // Where a workgroup's share of all requests' steps begins: request b, step `at` of it; `left` steps long (0: nothing), `per` being the
 // shares' length.
@@ -149,7 +154,8 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     return s;
 }
 
-// Waves on a SIMD that the registers are cut to: as many as fit without scratch memory.  Two at least, so that there are 256 vector
+// Waves on a SIMD that the registers are cut to: as many as fit without scratch memory (fp32 rows of 256 values keep 24 bytes of it, outside
+// the loop over tiles).  Two at least, so that there are 256 vector
 // registers and no accumulation registers: copies out of those have come ahead of the matrix instructions' results here (a branch right
 // behind the last product: clang 20 leaves out the wait states on its way), which the build checks there are none of.
 template <int DP, bool FP8, int NT, bool F32Q>
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         }
         const int RG = nrows * a.G - x0;      // query rows from x0 on
         if (RG <= 0 || take <= 0) continue;
-        const int t0 = at_step * kAttendLeast, t1 = complete ? len : min(len, t0 + take * kAttendLeast);
+        const int t0 = at_step * kAttendStep, t1 = complete ? len : min(len, t0 + take * kAttendStep);
         const int64_t kept_at = ((int64_t)blockIdx.x * a.places + place) * 2 + (segment != 0);
 
         // q's operand: row x0 + 16 nt + m is head h G + (x0_head + 16 nt + m) % G of new token x0_row + (x0_head + 16 nt + m) / G; the

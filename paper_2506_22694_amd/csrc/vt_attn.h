@@ -83,7 +83,7 @@ hipError_t launch_attend(const AttendArgs &a, bool f32, hipStream_t st);
 
 constexpr int kAttendWaves = 4;
 constexpr int kAttendTile = 32;                                   // cached tokens that a wave takes at a time
-constexpr int kAttendLeast = kAttendWaves * kAttendTile;          // ... and a workgroup: the steps that requests are cut up by
+constexpr int kAttendStep = kAttendWaves * kAttendTile;          // ... and a workgroup: the steps that requests are cut up by
 
 // csrc/vt_attend_d*.hip
 hipError_t launch_attend_d64(const AttendArgs &a, int tiles, bool f32, hipStream_t st);

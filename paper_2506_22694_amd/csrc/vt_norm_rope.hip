@@ -3,6 +3,9 @@
 // A head row is spread over GL = 8, 16 or 32 lanes (head_dim <= 64, 128, 256), eight values each: the four pairs the lane rotates, or
 // eight values past the rotated ones.  So a pair never leaves its lane, and the sum of squares is the only thing that does (three to five
 // DPP steps).  A lane keeps its values in fp32 from the load to the one rounding at the store.
+//
+// Bound by the bytes read and written: 4096 rows of 40 heads of 128 values in bf16 (84 MB) 16.5 us, 16384 rows 68 us, 4.9 TB/s, a copy's rate
+// of as much; gradients of 8192 rows (252 MB) 51 us and 4.6 for the weights' sums; 65537 rows of 8 heads read back from 8 bits (404 MB) 76 us.
 #include "vt_values.h"
 
 namespace vt {
@@ -137,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
     }
     for (int64_t row = ((int64_t)blockIdx.x << log2) + (SEVERAL ? group / per : 0); row < a.n; row += gridDim.x << log2) {
         for (int base = own; base < heads; base += kRowsAhead * per) {
-            // all of a group's rows of the token at a time: 16 bytes a lane would leave too little under way
+            // all of a group's rows of the token at a time: a row's 16 bytes a lane leave too little under way (8192 rows into the cache 48 us, 40 so)
             Raw8<T> raw[kRowsAhead] = {};
 #pragma unroll
             for (int u = 0; u < kRowsAhead; ++u) {
