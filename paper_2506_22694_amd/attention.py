@@ -106,7 +106,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     the row's position: (q', k') in their type.  Without weights no norm, without a table no rotation.
 
     `q_out` / `k_out` supply the results (q and k themselves, say).  Where a gradient is asked for, it comes from
-    qk_norm_rope_backward."""
+    qk_norm_rope_backward; a program that captures its backward pass in a graph calls that itself."""
     if binding._bind is not None:
         got = binding._bind.norm(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
         if got is not None:
