@@ -28,7 +28,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
     // (every place has said what it begins; a request only if it has rows: nothing of one without is looked at)
     const int4 parts = a.part_at[b];
     if (a.by_place) b = parts.w;
-    int64_t first;
+    int first;
     if (r >= rows_of(a.row_start, b, a.n, a.max_rows, first) || parts.y == 1) return;
     const int h = head / a.G, rows = 16 * a.row_tiles, x = r * a.G + head - h * a.G, rb = x / rows;
     const int64_t at = ((int64_t)(rb * a.cache.heads + h) * a.places + parts.x) * 2 * rows + (x - rb * rows);
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
     const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] *= inverse;
-    store_values(a, (first + r) * a.out_stride + head * a.cache.D + d, o, F32Q);
-    if (d == 0 && a.lse != nullptr) a.lse[(first + r) * a.hq + head] = log_sum_exp(top, total);
+    store_values(a, (int64_t)(first + r) * a.out_stride + head * a.cache.D + d, o, F32Q);
+    if (d == 0 && a.lse != nullptr) a.lse[(int64_t)(first + r) * a.hq + head] = log_sum_exp(top, total);
 }
 
 template <int LV, int TEAM>

@@ -242,12 +242,12 @@ int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int
     if (split.bytes > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < split.bytes)) return VT_ERR_WORKSPACE;
     if (!aligned(out_lse, 4)) return VT_ERR_ALIGN;
     vt::AttendArgs a{};
-    a.q = q, a.q_stride = q_stride, a.n = n, a.hq = q_heads, a.G = q_heads / cache->heads;
+    a.q = q, a.q_stride = q_stride, a.n = (int)n, a.hq = q_heads, a.G = q_heads / cache->heads;
     a.cache = cache_args(*cache);
     a.page_table = page_table, a.table_pages = table_pages, a.lengths = lengths, a.requests = n_requests;
     a.row_start = row_start, a.max_rows = max_rows, a.tail_mask = tail_mask;
     const int64_t held = (int64_t)table_pages * cache->page_size;
-    a.most = max_length < held ? max_length : held;
+    a.most = (int)(max_length < held ? max_length : held);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.out = out, a.out_stride = out_stride, a.lse = out_lse;
     a.whole = split.whole, a.places = split.places, a.row_blocks = split.row_blocks, a.row_tiles = split.row_tiles;

@@ -105,9 +105,9 @@ struct Request {
     int tokens, rows, first;
 };
 __device__ __forceinline__ Request request_of(const AttendArgs &a, int b) {
-    int64_t first;
+    int first;
     const int rows = rows_of(a.row_start, b, a.n, a.max_rows, first);
-    return {tokens_of(a.lengths[b], a.most), rows, (int)first};
+    return {tokens_of(a.lengths[b], a.most), rows, first};
 }
 __device__ __forceinline__ int request_steps(const Request &r) { return steps_of(r.tokens, r.rows, kAttendStep); }
 
@@ -226,7 +226,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         const int RG = nrows * a.G - x0;      // query rows from x0 on
         if (RG <= 0 || take <= 0) continue;
         const int t0 = at_step * kAttendStep, t1 = complete ? len : min(len, t0 + take * kAttendStep);
-        const int64_t kept_at = ((int64_t)blockIdx.x * a.places + place) * 2 + (segment != 0);
+        const int64_t kept_at = (((int64_t)blockIdx.x * a.places + place) * 2 + (segment != 0)) * (16 * NT);
+        float *const kept_o = a.part_o + kept_at * D;
+        float2 *const kept_ms = a.part_ms + kept_at;
 
         // q's operand: row x0 + 16 nt + m is head h G + (x0_head + 16 nt + m) % G of new token x0_row + (x0_head + 16 nt + m) / G; the
         // values of d that the lane's K has
@@ -608,7 +610,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
             }
             if (wave == 0 && g == 0 && 16 * nt + m < RG) {
                 const int y = x0_head + 16 * nt + m, up = by_group(a, y);
-                if (!complete) a.part_ms[kept_at * (16 * NT) + 16 * nt + m] = make_float2(most, all);
+                if (!complete) kept_ms[16 * nt + m] = make_float2(most, all);
                 else if (a.lse != nullptr) a.lse[(first + x0_row + up) * a.hq + h * a.G + y - up * a.G] = log_sum_exp(most, all);
             }
         }
@@ -628,7 +630,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                 for (int i = 0; i < 4; ++i) o[i] += u[i];
             }
             if (!complete) {
-                F32::store4(a.part_o + (kept_at * (16 * NT) + x) * D + d, o);
+                F32::store4(kept_o + (x * D + d), o);
                 continue;
             }
             const int y = x0_head + x, up = by_group(a, y);

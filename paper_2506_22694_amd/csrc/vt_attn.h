@@ -53,8 +53,8 @@ hipError_t launch_cache_read(const CacheReadArgs &a, bool bf16, hipStream_t st);
 
 struct AttendArgs {
     const void *q;
-    int64_t q_stride, n;
-    int hq, G;      // query heads, and how many share a kv head
+    int64_t q_stride;
+    int n, hq, G;      // query heads, and how many share a kv head
     CacheArgs cache;
     const int32_t *page_table;
     int table_pages;
@@ -63,7 +63,7 @@ struct AttendArgs {
     const int32_t *row_start;
     int max_rows;
     const uint64_t *tail_mask;
-    int64_t most;      // tokens of a request that are looked at
+    int most;          // tokens of a request that are looked at
     float scale_log2;
     void *out;
     int64_t out_stride;

@@ -23,19 +23,19 @@ VT_BOTH int64_t row_of_page(int page, int64_t pages, int heads, int head, int pa
     return ((int64_t)page * heads + head) << page_shift;
 }
 // Cached tokens of a request that are looked at.
-VT_BOTH int tokens_of(int length, int64_t most) { return length < 0 ? 0 : length > most ? (int)most : length; }
+VT_BOTH int tokens_of(int length, int most) { return length < 0 ? 0 : length > most ? most : length; }
 
 // New rows of request b: the first one in `first`; none where row_start is out of order or past the n rows there are.
-VT_BOTH int rows_of(const int32_t *row_start, int b, int64_t n, int max_rows, int64_t &first) {
+VT_BOTH int rows_of(const int32_t *row_start, int b, int n, int max_rows, int &first) {
     if (row_start == nullptr) {
         first = b;
         return 1;
     }
     first = row_start[b];
-    int64_t end = row_start[b + 1];
+    int end = row_start[b + 1];
     if (end > n) end = n;
     if (first < 0 || end <= first) return 0;
-    return end - first > max_rows ? max_rows : (int)(end - first);
+    return end - first > max_rows ? max_rows : end - first;
 }
 
 // Requests are taken in steps of `step` tokens; one without tokens has one too, for its rows' results.

@@ -168,8 +168,8 @@ _CELLS = r"""
 extern "C" {
 int64_t slot(int64_t s, int64_t pages, int heads, int head, int shift) { return vt::row_of_slot(s, pages, heads, head, shift); }
 int64_t page(int p, int64_t pages, int heads, int head, int shift) { return vt::row_of_page(p, pages, heads, head, shift); }
-int tokens(int length, int64_t most) { return vt::tokens_of(length, most); }
-int rows(const int32_t *start, int b, int64_t n, int max_rows, int64_t *first) { return vt::rows_of(start, b, n, max_rows, *first); }
+int tokens(int length, int most) { return vt::tokens_of(length, most); }
+int rows(const int32_t *start, int b, int n, int max_rows, int *first) { return vt::rows_of(start, b, n, max_rows, *first); }
 int steps(int tokens, int rows, int step) { return vt::steps_of(tokens, rows, step); }
 int share(int all, int places, int place, int *per, int *start) { return vt::share_steps(all, places, place, *per, *start); }
 int exponent(float x) { uint32_t u; __builtin_memcpy(&u, &x, 4); return vt::scale_exponent(u); }
@@ -187,8 +187,8 @@ def cells(tmp_path_factory):
     i64, i32 = ctypes.c_int64, ctypes.c_int32
     L.slot.argtypes, L.slot.restype = [i64, i64, i32, i32, i32], i64
     L.page.argtypes, L.page.restype = [i32, i64, i32, i32, i32], i64
-    L.tokens.argtypes = [i32, i64]
-    L.rows.argtypes = [ctypes.c_void_p, i32, i64, i32, ctypes.POINTER(i64)]
+    L.tokens.argtypes = [i32, i32]
+    L.rows.argtypes = [ctypes.c_void_p, i32, i32, i32, ctypes.POINTER(i32)]
     L.share.argtypes = [i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
     L.exponent.argtypes = [ctypes.c_float]
     return L
@@ -214,7 +214,7 @@ def test_slots_and_pages_outside_the_cache_have_no_row(cells):
 def test_lengths_and_rows_stay_within_what_there_is(cells):
     assert [cells.tokens(x, 100) for x in (-(1 << 31), -1, 0, 1, 100, 101, (1 << 31) - 1)] == [0, 0, 0, 1, 100, 100, 100]
     assert cells.tokens((1 << 31) - 1, 1 << 30) == 1 << 30
-    first = ctypes.c_int64()
+    first = ctypes.c_int32()
     assert cells.rows(None, 5, 6, 1, ctypes.byref(first)) == 1 and first.value == 5
     start = (ctypes.c_int32 * 9)(0, 3, 3, 10, 9, -4, 2, 50, 60)
     got = []
