@@ -17,7 +17,9 @@
 // 8-bit caches: codes become bf16 (exactly) on their way, two for each conversion; scales are powers of two and go on the scores
 // and on p, where they are exact as well.
 //
-// fp32 rows: a value of 24 bits is the sum of three of 8, so q and p are three operands each, and products are exact as for bf16.  bf16
+// fp32 rows: a value of 24 bits is the sum of three of 8, so q and p are three operands each, and products are exact as for bf16.  An infinity
+// on the other side is still one after three products only if all three terms have the value's sign and none is zero: the first two are
+// cut off from just below what they are taken of.  bf16
 // rows have p rounded to bf16 once, after their sum was taken: with two operands for it results are off by 0.0017 instead of 0.0020 of
 // their size (0.0017 is their own rounding), and take up to 2.5 % longer.
 //
@@ -57,26 +59,24 @@ __device__ __forceinline__ float half_sum(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-// What is left of a value after its leading 8 bits
-__device__ __forceinline__ float less_bf16(float x, float &leading) {
-    leading = (float)(__bf16)x;
-    return x - leading;
-}
-
-// Eight fp32 values as the sum of three operands
-__device__ __forceinline__ void split_terms(u32x4 a, u32x4 b, u32x4 (&terms)[3]) {
-    float v[8], lead[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(a[j]), v[4 + j] = __uint_as_float(b[j]);
+// Eight fp32 values (none -0) as the sum of three operands: the leading 8 bits of what is just below the value, those of what is just below the
+// rest, and the rest, which has 8.  (Below it by the last of its 24 bits; below an infinity are the largest finite ones.  0 is three zeros.)
+template <typename Terms>
+__device__ __forceinline__ void split_terms(float (&v)[8], Terms &terms) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
+        unsigned u[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = less_bf16(v[j], lead[j]);
-        terms[i] = u32x4{pack_bf16(lead[0], lead[1]), pack_bf16(lead[2], lead[3]), pack_bf16(lead[4], lead[5]), pack_bf16(lead[6], lead[7])};
+        for (int j = 0; j < 8; ++j) {
+            u[j] = __float_as_uint(v[j]);
+            if (i == 2) continue;
+            u[j] = __builtin_elementwise_sub_sat(u[j], 1u);
+            v[j] -= __uint_as_float(u[j] & 0xFFFF0000u);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) terms[i][j] = __builtin_amdgcn_perm(u[2 * j + 1], u[2 * j], 0x07060302);
     }
 }
-template <int TERMS>
-__device__ __forceinline__ void split_terms(u32x4, u32x4, u32x4 (&)[TERMS]) {}
 
 constexpr float kNone = -__builtin_inff();
 
@@ -247,7 +247,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                 for (int i = 0; i < (F32Q ? 2 : 1); ++i) {
                     const u32x4 u = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.q) + from * (F32Q ? 4 : 2) + 16 * i);
-                    q[nt][(F32Q ? 2 : 1) * s + i] = there ? u : u32x4{0, 0, 0, 0};
+                    u32x4 &to = q[nt][(F32Q ? 2 : 1) * s + i];
+                    to = there ? u : u32x4{0, 0, 0, 0};
+                    if constexpr (F32Q) {      // (-0 is 0)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) to[j] = __float_as_uint(__uint_as_float(to[j]) + 0.0f);
+                    }
                 }
             }
         }
@@ -415,8 +420,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         if constexpr (F32Q) asm volatile("" : "+v"(q[nt][2 * c]), "+v"(q[nt][2 * c + 1]));      // (split here, not ahead of the loop)
-                        if constexpr (F32Q) split_terms(q[nt][2 * c], q[nt][2 * c + 1], terms[nt]);
-                        else terms[nt][0] = q[nt][c];
+                        if constexpr (F32Q) {
+                            float x[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(q[nt][2 * c + j / 4][j % 4]);
+                            split_terms(x, terms[nt]);
+                        } else {
+                            terms[nt][0] = q[nt][c];
+                        }
                     }
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -515,16 +526,11 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                         for (int j = 0; j < 8; ++j) w[j] *= scale_of((v_scale[j / 4] >> 8 * (j % 4)) & 0xFF);
                     }
+                    if constexpr (TERMS > 1) {
+                        split_terms(w, p[nt]);
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < TERMS; ++e) {
-                        float lead[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if constexpr (TERMS > 1) w[j] = less_bf16(w[j], lead[j]);
-                            else lead[j] = w[j];
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) p[nt][e][j] = pack_bf16(lead[2 * j], lead[2 * j + 1]);
+                        for (int j = 0; j < 4; ++j) p[nt][0][j] = pack_bf16(w[2 * j], w[2 * j + 1]);
                     }
                 }
                 if (ends) {

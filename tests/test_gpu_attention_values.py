@@ -1,0 +1,76 @@
+"""Attention of values where sums of bf16 terms, scales and masks can go wrong: infinities on either side, weights that bf16 does not hold, scale
+bytes at the ends of their range.  Against the definitions in 64 bits, with the tolerances of test_gpu_attention.py."""
+import math
+
+import pytest
+import torch
+
+import paper_2506_22694_amd as vt
+from test_gpu_attention import BF16, E4M3, F32, _case, _check_attention, _gen, _randn
+
+pytestmark = pytest.mark.gpu
+
+
+def _place(table, page, token, b=0):
+    return table[b, token // page].long(), token % page
+
+
+# ---------------------------------------------------------------------------------------------- infinities that rows see
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("length", [5, 300, 3000])      # (a request taken whole, and in shares)
+def test_scores_of_minus_infinity(D, dtype, length):
+    """Keys of -inf under positive queries: tokens as if not seen; all of them: nothing is seen."""
+    g = _gen(D + length)
+    hk, page = 2, 16
+    cache, table, lengths, q, _ = _case(g, BF16, dtype, 4, hk, D, page, [length, length])
+    q = q.abs()
+    for token in {0, length // 2, length - 1} - {1}:
+        page_id, at = _place(table, page, token)
+        cache.k[page_id, :, at] = -math.inf
+        cache.k[page_id, 0, at, 1:] = cache.k[page_id, 0, at, 1:].clamp(min=0.0)      # (of one head one value only)
+    out, lse = _check_attention(cache, table, lengths, q, None)
+    assert out.isfinite().all() and lse.isfinite().all()
+    cache.k.fill_(-math.inf)
+    out, lse = vt.paged_attention(q, cache, table, lengths, return_lse=True)
+    assert out.eq(0).all() and lse.eq(-math.inf).all()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("held", [BF16, E4M3])
+def test_queries_of_infinity_and_the_largest_values(D, dtype, held):
+    g = _gen(D)
+    cache, table, lengths, q, _ = _case(g, held, dtype, 4, 2, D, 16, [200, 1000])
+    k = cache.k.view(torch.uint8) if held == E4M3 else cache.k
+    k[..., 3] = 0xB8 if held == E4M3 else -1.0      # -1 in e4m3
+    q[0, 1, 3] = math.inf      # every score is -inf
+    q[1, 2, 3] = -math.inf      # ... +inf, which has no weights
+    out, lse = vt.paged_attention(q, cache, table, lengths, return_lse=True)
+    assert out[0, 1].eq(0).all() and lse[0, 1] == -math.inf
+    assert out[1, 2].isnan().all() and out[0, 0].isfinite().all() and out[1, 3].isfinite().all()
+    # the largest finite values, on keys that bring them back to scores of some size
+    if held == BF16:
+        q[0, 1, 3] = q[1, 2, 3] = torch.finfo(dtype).max
+        cache.k[..., 3] = (_randn(g, *cache.k.shape[:3]) * 2.0 ** -126).to(BF16)
+        _check_attention(cache, table, lengths, q, None)
+
+
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [None, [2, 9]])
+def test_values_of_infinity_and_nan_that_all_rows_see(D, dtype, rows):
+    """... reach their own column of the result and no other, before the last 64 tokens and among them, with a mask or without."""
+    g = _gen(D)
+    hk, page = 2, 32
+    cache, table, lengths, q, starts = _case(g, BF16, dtype, 8, hk, D, page, [2100, 350], rows=rows)
+    for b, token, head, d, value in ((0, 70, 0, 5, math.inf), (0, 71, 0, 5, math.inf), (0, 2099, 0, 6, -math.inf), (0, 1000, 1, 7, math.nan), (1, 3, 1, 11, -math.inf),
+                                     (1, 9, 0, 2, math.inf), (1, 349, 0, 2, -math.inf), (1, 349, 0, 12, math.inf)):      # (of both signs: NaN)
+        page_id, at = _place(table, page, token, b)
+        cache.v[page_id, head, at, d] = value
+    n = q.shape[0]
+    for mask in (None, torch.full((n,), -1, device="cuda")):
+        out, lse = _check_attention(cache, table, lengths, q, starts, mask=mask)
+        assert lse.isfinite().all()
+        assert out[-1, 4:, 11].eq(-math.inf).all() and out[-1, :4, 2].isnan().all() and out[0, :4, 5].eq(math.inf).all() and out[0, 4:, 7].isnan().all()
+        assert out[0].isfinite().sum() == 8 * D - 12 and out[-1].isfinite().sum() == 8 * D - 12
