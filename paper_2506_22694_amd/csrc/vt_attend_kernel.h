@@ -17,11 +17,11 @@
 // 8-bit caches: codes become bf16 (exactly) on their way, two for each conversion; scales are powers of two and go on the scores
 // and on p, where they are exact as well.
 //
-// fp32 rows: a value of 24 bits is the sum of three of 8, so q and p are three operands each, and products are exact as for bf16.  An infinity
-// on the other side is still one after three products only if all three terms have the value's sign and none is zero: the first two are
-// cut off from just below what they are taken of.  bf16
-// rows have p rounded to bf16 once, after their sum was taken: with two operands for it results are off by 0.0017 instead of 0.0020 of
-// their size (0.0017 is their own rounding), and take up to 2.5 % longer.
+// Values of 24 bits -- the weights p, and q of fp32 rows -- are sums of three of 8, so they are three operands each, and products are exact as
+// for bf16.  An infinity on the other side is still one after three products only if all three terms have the value's sign and none is
+// zero: the first two are cut off from just below what they are taken of.  (p as one operand, rounded to bf16: results in bf16 off by 0.0018
+// to 0.0021 of their size instead of 0.0016 to 0.0017, their own rounding; 131001 tokens as long, 64 tree levels of 8 nodes 83 instead of 84 us, over
+// 8 bits 61 instead of 65, 16 nodes of 64 heads of 64 values 71 instead of 81.)
 //
 // 131001 tokens of one request, 8 kv heads of 128 values in bf16, 4 query heads each: 537 MB in 80 us, 6.7 TB/s, where a plain read of as much
 // takes 79; 151 vector and 16 matrix instructions a tile (8 bits: 268 and 16; 48 ragged requests 541 MB in 94 us, 5.8 TB/s).
@@ -166,7 +166,7 @@ constexpr int attend_occupancy() {
 
 template <int DP, bool FP8, int NT, bool F32Q>
 __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F32Q>())) void attend_kernel(AttendArgs a) {
-    constexpr int W = kAttendWaves, E = DP / 16, KS = DP / 32, TERMS = F32Q ? 3 : 1;
+    constexpr int W = kAttendWaves, E = DP / 16, KS = DP / 32, TERMS = F32Q ? 3 : 1;      // (of q)
     constexpr int KL = FP8 ? DP / 64 : DP / 32;       // 16-byte loads of a token's row of K in a lane
     constexpr int VR = FP8 ? DP / 64 : DP / 32;       // registers of a token's E values of V
     constexpr int SZ = FP8 ? 1 : 2;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 
         // NaN and infinities among values that some row does not see: 0 * inf must not reach it.  They are taken out of V, and counted in products
         // of ones for each row that sees them, whose sums become what they would have.
-        unsigned p[NT][TERMS][4], sees[NT][4];
+        unsigned p[NT][3][4], sees[NT][4];
         auto take_out_odd = [&]() {
 #pragma unroll
             for (int r = 0; r < VR; ++r) {
@@ -526,12 +526,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                         for (int j = 0; j < 8; ++j) w[j] *= scale_of((v_scale[j / 4] >> 8 * (j % 4)) & 0xFF);
                     }
-                    if constexpr (TERMS > 1) {
-                        split_terms(w, p[nt]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) p[nt][0][j] = pack_bf16(w[2 * j], w[2 * j + 1]);
-                    }
+                    split_terms(w, p[nt]);
                 }
                 if (ends) {
                     // what lies past the end may be anything, NaN too
@@ -560,11 +555,11 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     u32x4 f[VF];
                     operands(r, f);
 #pragma unroll
-                    for (int i = 0; i < VF; ++i) {
+                    for (int e = 2; e >= 0; --e) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
+                        for (int i = 0; i < VF; ++i) {
 #pragma unroll
-                            for (int e = TERMS - 1; e >= 0; --e)
+                            for (int nt = 0; nt < NT; ++nt)
                                 acc[nt][VF * r + i] = mfma(f[i], u32x4{p[nt][e][0], p[nt][e][1], p[nt][e][2], p[nt][e][3]}, acc[nt][VF * r + i]);
                         }
                     }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2506_22694_amd as vt
-from test_gpu_attention import BF16, E4M3, F32, _case, _check_attention, _gen, _randn
+from test_gpu_attention import BF16, E4M3, F32, _case, _check_attention, _gen, _randn, _values, attend64
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,45 @@ def test_values_of_infinity_and_nan_that_all_rows_see(D, dtype, rows):
         assert lse.isfinite().all()
         assert out[-1, 4:, 11].eq(-math.inf).all() and out[-1, :4, 2].isnan().all() and out[0, :4, 5].eq(math.inf).all() and out[0, 4:, 7].isnan().all()
         assert out[0].isfinite().sum() == 8 * D - 12 and out[-1].isfinite().sum() == 8 * D - 12
+
+
+# ---------------------------------------------------------------------------------------------- weights of 24 bits
+def test_weights_that_bf16_does_not_hold():
+    """One token of weight 1, all others just above 1/2 and off by the same part of it in bf16; values of 1: the result is 1."""
+    cache, table, lengths, q, _ = _case(_gen(1), BF16, BF16, 4, 2, 64, 16, [40, 300, 3000])
+    cache.k.zero_()
+    cache.v.fill_(1.0)
+    cache.k[..., 0] = 1.0
+    for b in range(3):
+        page_id, at = _place(table, 16, 7, b)
+        cache.k[page_id, :, at] = 0.0
+    q.zero_()
+    q[..., 0] = 1.0
+    out = vt.paged_attention(q, cache, table, lengths, scale=math.log(0.5 + 0.9 * 2.0 ** -9))
+    assert out.eq(1.0).all()
+
+
+@pytest.mark.parametrize("hq,hk,D", [(4, 2, 64), (32, 8, 128), (6, 3, 256), (40, 1, 64), (12, 2, 96)])
+@pytest.mark.parametrize("held", [BF16, E4M3])
+@pytest.mark.parametrize("rows", [None, [5, 2, 8]])
+def test_results_of_bf16_rows_are_rounded_once(hq, hk, D, held, rows):
+    g = _gen(hq + D)
+    cache, table, lengths, q, starts = _case(g, held, BF16, hq, hk, D, 32, [333, 2222, 64], rows=rows)
+    mask = None if rows is None else torch.randint(-(1 << 63), (1 << 63) - 1, (15,), generator=g, device="cuda") | 1
+    out = vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=1 if rows is None else 8, tail_mask=mask)
+    first = [0, 1, 2, 3] if rows is None else starts.tolist()
+    for b, length in enumerate(lengths.tolist()):
+        at = slice(first[b], first[b + 1])
+        k, v = _values(cache, table, b, length)
+        see = torch.ones(first[b + 1] - first[b], length, dtype=torch.bool, device="cuda")
+        if mask is not None:
+            bit = torch.arange(length, device="cuda") - (length - 64)
+            see &= (bit < 0) | (mask[at][:, None] >> bit.clamp(min=0) & 1).bool()
+        want = attend64(q[at], k, v, see, D ** -0.5)[0]
+        # half a step at the value itself, and fp32's part: scores off by (sqrt(D) / 2 + 8) half steps of the sum of their products' sizes, and 40 for
+        # exp2 and the sums, as a part of every weight, above and below the line
+        sizes = (q[at].double().abs()[:, None] * k.abs().repeat_interleave(hq // hk, 1)[None]).sum(-1).max().item() * D ** -0.5
+        fp32 = (sizes * (math.sqrt(D) / 2 + 8) + 40) * 2.0 ** -24
+        half = torch.ldexp(torch.ones_like(want), torch.frexp(want).exponent - 9)
+        off = (out[at].double() - want).abs() - half - 2 * fp32 * attend64(q[at], k, v.abs(), see, D ** -0.5)[0]
+        assert off.max().item() <= 0.0
