@@ -78,7 +78,9 @@ size_t vt_qk_norm_rope_backward_ws_bytes(int64_t n, int32_t head_dim);
  *
  *   k, v              [pages, heads, page_size, head_dim] of type VT_BF16 or VT_E4M3
  *   k_scale, v_scale  [pages, heads, page_size] exponents of the scales, VT_E4M3
- *                     only (else NULL): code c stands for c * 2^(scale - 127)
+ *                     only (else NULL): code c stands for c * 2^(scale - 127).  (255 has
+ *                     no place in fp32 but for the least codes: what reads or sees such
+ *                     a token may get infinities and NaN.)
  *   page_size         a power of two, 16 .. 65536
  *   head_dim          a multiple of 16, <= VT_MAX_HEAD_DIM
  *
@@ -124,8 +126,10 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *   s[t] = scale * sum_d q[i, h, d] * k[t, g, d]    over the tokens t that row i sees
  *   out[i, h, :] = sum_t exp(s[t] - lse) * v[t, g, :],   lse[i, h] = log sum_t exp(s[t])
  *
- * in fp32.  A row that sees nothing (or whose scores are all -inf) has out = 0 and
- * lse = -inf.  What a row does not see does not reach it, NaN and infinities included.
+ * in fp32 (a weight times an 8-bit row's scale counts as less, or not at all, below
+ * 2^-126).  A row that sees nothing (or whose scores are all -inf) has out = 0 and
+ * lse = -inf.  What a row does not see does not reach it, NaN, infinities and any scale
+ * included.
  *
  *   q, out       [n, q_heads, head_dim], type VT_BF16 or VT_F32; n <= n_requests * max_rows
  *   page_table   [n_requests, table_pages] int32; entries past a request's tokens are

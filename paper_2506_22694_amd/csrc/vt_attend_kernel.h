@@ -450,7 +450,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                 for (int t = 0; t < 2; ++t) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        factor[t][i] = FP8 ? scale_of((k_scale[t] >> 8 * i) & 0xFF) * a.scale_log2 : a.scale_log2;
+                        factor[t][i] = FP8 ? scaled(a.scale_log2, (k_scale[t] >> 8 * i) & 0xFF) : a.scale_log2;
                 }
 
                 // the next tile's keys are asked for once this one's are used up, its values likewise below
@@ -468,10 +468,6 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     for (int t = 0; t < 2; ++t) {
                         const int left = t1 - (token + 16 * t + 4 * g);
                         there[t] = row[t] < 0 || left <= 0 ? 0u : left >= 4 ? 15u : (1u << left) - 1u;
-                    }
-                    if constexpr (FP8) {      // (a scale of what lies past the end may be infinite, and p = 0 there)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v_scale[j / 4] &= (there[j / 4] >> j % 4) & 1 ? ~0u : ~(0xFFu << 8 * (j % 4));
                     }
                 }
 #pragma unroll
@@ -524,7 +520,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     }
                     if constexpr (FP8) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) w[j] *= scale_of((v_scale[j / 4] >> 8 * (j % 4)) & 0xFF);
+                        for (int j = 0; j < 8; ++j) w[j] = scaled(w[j], (v_scale[j / 4] >> 8 * (j % 4)) & 0xFF);      // (0 stays, whatever is held)
                     }
                     split_terms(w, p[nt]);
                 }

@@ -115,7 +115,7 @@ __device__ __forceinline__ void to_cache(const CacheArgs &c, bool is_v, int64_t 
     const int e = scale_exponent(__float_as_uint(m));
     if (!l.active || cell < 0) return;
     // (a value next to fp32's largest would be rounded up to 256 * 2^120, which is infinite)
-    const float inverse = scale_of(254 - e), most = e == 247 ? 240.0f : 448.0f;
+    const float inverse = __uint_as_float((unsigned)(254 - e) << 23), most = e == 247 ? 240.0f : 448.0f;
     uint8_t *p = static_cast<uint8_t *>(is_v ? c.v : c.k) + cell * c.D;
     *reinterpret_cast<unsigned *>(p + l.o0) = pack_e4m3(x, inverse, most);
     *reinterpret_cast<unsigned *>(p + l.o1) = pack_e4m3(x + 4, inverse, most);
@@ -314,12 +314,12 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a) {
                     Bf16::load4(p + 4, x + 4);
                 } else {
                     const u32x2 u = *reinterpret_cast<const u32x2 *>(static_cast<const uint8_t *>(held) + cell * a.cache.D + o);
-                    const float s = scale_of((which ? a.cache.v_scale : a.cache.k_scale)[cell]);
+                    const unsigned e = (which ? a.cache.v_scale : a.cache.k_scale)[cell];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int w = (int)(j ? u.y : u.x);
                         const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                        x[4 * j] = lo[0] * s, x[4 * j + 1] = lo[1] * s, x[4 * j + 2] = hi[0] * s, x[4 * j + 3] = hi[1] * s;
+                        x[4 * j] = scaled(lo[0], e), x[4 * j + 1] = scaled(lo[1], e), x[4 * j + 2] = scaled(hi[0], e), x[4 * j + 3] = scaled(hi[1], e);
                     }
                 }
             }

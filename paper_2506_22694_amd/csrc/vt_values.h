@@ -83,6 +83,7 @@ __device__ __forceinline__ unsigned pack_e4m3(const float *x, float inverse, flo
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
 }
-__device__ __forceinline__ float scale_of(int exponent) { return __uint_as_float((unsigned)exponent << 23); }
+// x * 2^(exponent - 127) for every byte that a cache may hold: as a float's exponent bits, 0 would be no 2^-127 and 255 would make NaN of x = 0
+__device__ __forceinline__ float scaled(float x, unsigned exponent) { return __builtin_ldexpf(x, (int)exponent - 127); }
 
 }  // namespace vt

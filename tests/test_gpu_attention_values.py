@@ -116,3 +116,59 @@ def test_results_of_bf16_rows_are_rounded_once(hq, hk, D, held, rows):
         half = torch.ldexp(torch.ones_like(want), torch.frexp(want).exponent - 9)
         off = (out[at].double() - want).abs() - half - 2 * fp32 * attend64(q[at], k, v.abs(), see, D ** -0.5)[0]
         assert off.max().item() <= 0.0
+
+
+# ---------------------------------------------------------------------------------------------- scale bytes at the ends of their range
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows", [2, 9])
+def test_hidden_tokens_may_hold_any_scale(D, dtype, rows):
+    """Tokens that a mask hides were never written: scales and codes of 255 there, beside tokens that are seen.  A row that sees one gets what
+    comes of it, the others nothing."""
+    g = _gen(D + rows)
+    hk, page, length = 2, 16, 150
+    cache, table, lengths, q, starts = _case(g, E4M3, dtype, 4, hk, D, page, [length, 70], rows=[rows, 2])
+    hidden = (1 << 64) - 1
+    for token, k_scale, v_scale, code in ((100, 255, 255, None), (101, 3, 255, 0x00), (117, 255, 3, 0x7F), (149, 255, 255, 0xFF), (140, 254, 255, 0x7E)):
+        page_id, at = _place(table, page, token)
+        cache.k_scale[page_id, :, at], cache.v_scale[page_id, :, at] = k_scale, v_scale
+        if code is not None:
+            cache.k.view(torch.uint8)[page_id, :, at] = code
+            cache.v.view(torch.uint8)[page_id, :, at] = code
+        hidden &= ~(1 << (token - length + 64))
+    mask = torch.full((rows + 2,), hidden - (hidden >> 63 << 64), device="cuda")
+    mask[rows:] = -1
+    want, _ = _check_attention(cache, table, lengths, q, starts, mask=mask)
+    assert want.isfinite().all()
+    mask[0] |= 1 << (101 - length + 64)
+    out = vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=rows, tail_mask=mask)
+    assert torch.equal(out[1:], want[1:])
+
+
+def test_every_scale_byte_reads_back_as_its_power_of_two():
+    page, D = 256, 16
+    codes = torch.tensor([0x00, 0x01, 0x07, 0x08, 0x38, 0x39, 0x7E, 0x7F, 0x80, 0x81, 0x87, 0x88, 0xB8, 0xB9, 0xFE, 0xFF], dtype=torch.uint8, device="cuda")
+    held = codes.expand(1, 1, page, D).contiguous()
+    scale = torch.arange(256, dtype=torch.uint8, device="cuda").view(1, 1, page)
+    cache = vt.KVCache.of(held.view(E4M3), held.clone().view(E4M3), scale, scale.clone())
+    powers = torch.tensor([math.ldexp(1.0, i - 127) for i in range(256)], dtype=torch.float64, device="cuda")
+    want = codes.view(E4M3).double()[None] * powers[:, None]
+    for got in vt.kv_cache_read(cache, torch.arange(page, device="cuda"), dtype=F32):
+        got = got[:, 0]
+        assert torch.equal(got.isnan(), want.isnan())
+        sure = (want == 0) | ((want.abs() >= 2.0 ** -126) & (want.abs() < 2.0 ** 128))
+        assert torch.equal(got.double()[sure], want[sure])
+        beyond = want.abs() >= 2.0 ** 128
+        assert torch.equal(got.double()[beyond], want[beyond].sign() * math.inf)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("byte", [0, 1, 60, 200])
+def test_attention_over_keys_of_any_scale(dtype, byte):
+    """Scores of one scale byte, brought back to some size by the scale of the call or by queries."""
+    g = _gen(byte)
+    cache, table, lengths, q, _ = _case(g, E4M3, dtype, 4, 2, 64, 32, [300, 1000])
+    cache.k_scale.fill_(byte)
+    near = max(min(127 - byte, 100), -100)      # of the scale of the call; the rest in the queries, whose own values fp32 holds
+    q = (q.double() * 2.0 ** (127 - byte - near)).to(dtype)
+    _check_attention(cache, table, lengths, q, None, scale=2.0 ** (near - 10))
