@@ -42,6 +42,13 @@ def _got(got):
     return got
 
 
+def _no_gradient(*tensors) -> None:
+    """Refuses what a gradient is asked for of, where there would be none."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
+        raise ValueError("no gradient comes back from here: detach what requires one, or call under torch.no_grad() (qk_norm_rope has gradients of q, k and "
+                         "the weights)")
+
+
 def _heads(t: torch.Tensor, n: int, heads: int, D: int, dtype) -> int:
     """The row stride of a tensor of heads, checked."""
     if not t.is_cuda or t.dtype != dtype or t.dim() != 3 or tuple(t.shape) != (n, heads, D):
@@ -111,6 +118,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
         got = binding._bind.norm(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
         if got is not None:
             return _got(got)
+    _no_gradient(table, q_out, k_out)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
         if q_out is not None or k_out is not None:
             raise ValueError("q_out and k_out are for calls without gradients")
@@ -138,7 +146,7 @@ def qk_norm_rope_backward(gq: torch.Tensor, gk: torch.Tensor, q: torch.Tensor, k
                           k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
                           dq: torch.Tensor | None = None, dk: torch.Tensor | None = None, ws: torch.Tensor | None = None):
     """Gradients of qk_norm_rope from those of its results, (dq, dk, dq_weight, dk_weight): the weights' in float32 [D] (None
-    without weights).  `dq` / `dk` supply the results (gq and gk themselves, say)."""
+    without weights).  `dq` / `dk` supply the results (gq and gk themselves, say).  They are numbers: no graph leads through here."""
     L = load_library()
     if binding._bind is not None and dq is None and dk is None and ws is None:
         got = binding._bind.norm_backward(gq, gk, q, k, positions, table, q_weight, k_weight, eps, interleaved)
@@ -203,6 +211,7 @@ class KVCache:
         for s in (k_scale, v_scale):
             if (s is not None) != coded or (coded and (s.shape != k.shape[:3] or s.dtype != torch.uint8)):
                 raise ValueError("k_scale and v_scale must be uint8 [pages, heads, page_size], of an 8-bit cache only")
+        _no_gradient(k, v)
         _require_cuda(k, v, k_scale, v_scale)
         self._tensors = (k, v, k_scale, v_scale)
         pages, heads, page_size, head_dim = k.shape
@@ -229,12 +238,13 @@ def qkv_to_cache(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, cache
                  k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
                  q_out: torch.Tensor | None = None):
     """qk_norm_rope on q and k, with k and v written to the cache at `slots` (outside it: not written), in one launch.
-    Returns q' (None without q)."""
+    Returns q' (None without q).  Inputs that require a gradient are refused: none comes back from a cache."""
     L = load_library()
     if binding._bind is not None and q is not None and type(cache) is KVCache:
         got = binding._bind.to_cache(q, k, v, cache._address, slots, positions, table, q_weight, k_weight, eps, interleaved, q_out)
         if got is not None:
             return _got(got)
+    _no_gradient(q, k, v, table, q_weight, k_weight, q_out)
     n, hk, D = k.shape
     if hk != cache.heads or D != cache.head_dim:
         raise ValueError("k and v must have the cache's heads")
@@ -267,6 +277,7 @@ def kv_cache_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torc
         got = binding._bind.cache_read(cache._address, slots, dtype == torch.float32)
         if got is not None:
             return _got(got)
+    _no_gradient(k_out, v_out)
     n = slots.numel()
     shape = (n, cache.heads, cache.head_dim)
     if k_out is None:
@@ -303,13 +314,15 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     page_table int32 [requests, pages of each], lengths int32 [requests].  Row i is request i's, or rows
     row_start[b] .. row_start[b + 1] - 1 are request b's, at most max_rows (other rows are not computed).  tail_mask (int64 [n], its bits): which of
     the last 64 tokens a row sees, bit j being token length - 64 + j.  scale: of the scores (head_dim^-1/2).
-    max_length: no request is longer (the page table's width, where it isn't given; near the longest is fastest)."""
+    max_length: no request is longer (the page table's width, where it isn't given; near the longest is fastest).
+    A q that requires a gradient is refused: there is none."""
     L = load_library()
     if binding._bind is not None and type(ws) is AttentionWorkspace and type(cache) is KVCache:
         got = binding._bind.attend(q, cache._address, page_table, lengths, row_start, max_rows, tail_mask, max_length, scale, ws.buf, out, return_lse,
                                    out_lse)
         if got is not None:
             return _got(got)
+    _no_gradient(q, out, out_lse)
     n, hq, D = q.shape
     _require_cuda(page_table, lengths, row_start, tail_mask, out_lse)
     if page_table.dtype != torch.int32 or page_table.dim() != 2 or lengths.dtype != torch.int32:

@@ -222,6 +222,11 @@ decltype(&vt_kv_cache_read) g_read = nullptr;
 decltype(&vt_paged_attention) g_attend = nullptr;
 
 bool given(PyObject *o) { return o != Py_None; }
+// A gradient is asked for of the tensor: autograd's business, or a refusal
+const at::Tensor &plain(const at::Tensor &t) {
+    if (c10::GradMode::is_enabled() && t.requires_grad()) throw NotPlain();
+    return t;
+}
 
 // A tensor of heads [n, heads, head_dim], its rows apart
 struct Heads {
@@ -231,7 +236,8 @@ struct Heads {
     int32_t heads = 0, D = 0;
     Heads() = default;
     explicit Heads(const at::Tensor &x) : t(x) {
-        if (!t.is_cuda() || t.dim() != 3 || (c10::GradMode::is_enabled() && t.requires_grad())) throw NotPlain();
+        plain(t);
+        if (!t.is_cuda() || t.dim() != 3) throw NotPlain();
         n = t.size(0);
         heads = int32(t.size(1));
         D = int32(t.size(2));
@@ -284,7 +290,7 @@ struct Norm {
     Norm(PyObject *const *a, const Heads &x) {
         if (given(a[0]) != given(a[1]) || given(a[2]) != given(a[3])) throw NotPlain();
         if (given(a[1])) {
-            const at::Tensor &t = operand(a[1]);
+            const at::Tensor &t = plain(operand(a[1]));
             if (t.scalar_type() != at::kFloat || t.dim() != 2) throw NotPlain();
             table = static_cast<const float *>(t.data_ptr());
             rows = t.size(0);
@@ -300,8 +306,8 @@ struct Norm {
         style = truth(a[5]) ? VT_ROPE_NEIGHBOURS : VT_ROPE_HALVES;
     }
     static const void *weight(PyObject *o, const Heads &x) {
-        const at::Tensor &t = operand(o);
-        if (t.scalar_type() != x.t.scalar_type() || t.numel() != x.D || (c10::GradMode::is_enabled() && t.requires_grad())) throw NotPlain();
+        const at::Tensor &t = plain(operand(o));
+        if (t.scalar_type() != x.t.scalar_type() || t.numel() != x.D) throw NotPlain();
         return t.data_ptr();
     }
 };
@@ -458,7 +464,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         const bool with_lse = truth(a[11]);
         at::Tensor lse;
         if (given(a[12])) {
-            lse = operand(a[12]);
+            lse = plain(operand(a[12]));
             if (lse.scalar_type() != at::kFloat || lse.numel() != q.n * q.heads) throw NotPlain();
         } else if (with_lse) {
             lse = at::empty({q.n, q.heads}, q.t.options().dtype(at::kFloat));
