@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 from .binding import VT_I32, VT_I64, _check, _dtype_code, _ptr, _require_cuda, _scratch, _stream, load_library
@@ -42,8 +43,17 @@ def _got(got):
     return got
 
 
+def _no_tangent(*tensors) -> None:
+    """Refuses dual tensors: no call here has a derivative in forward mode."""
+    if getattr(forward_ad, "_current_level", 0) < 0:      # (most often: no level is open, so there are none; 2.8 us a call to ask the tensors)
+        return
+    if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("no tangent comes back from here: there is no derivative in forward mode")
+
+
 def _no_gradient(*tensors) -> None:
     """Refuses what a gradient is asked for of, where there would be none."""
+    _no_tangent(*tensors)
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
         raise ValueError("no gradient comes back from here: detach what requires one, or call under torch.no_grad() (qk_norm_rope has gradients of q, k and "
                          "the weights)")
@@ -113,12 +123,13 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     the row's position: (q', k') in their type.  Without weights no norm, without a table no rotation.
 
     `q_out` / `k_out` supply the results (q and k themselves, say).  Where a gradient is asked for, it comes from
-    qk_norm_rope_backward; a program that captures its backward pass in a graph calls that itself."""
+    qk_norm_rope_backward (there is no forward mode); a program that captures its backward pass in a graph calls that itself."""
     if binding._bind is not None:
         got = binding._bind.norm(q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out)
         if got is not None:
             return _got(got)
     _no_gradient(table, q_out, k_out)
+    _no_tangent(q, k, q_weight, k_weight)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
         if q_out is not None or k_out is not None:
             raise ValueError("q_out and k_out are for calls without gradients")
@@ -152,6 +163,7 @@ def qk_norm_rope_backward(gq: torch.Tensor, gk: torch.Tensor, q: torch.Tensor, k
         got = binding._bind.norm_backward(gq, gk, q, k, positions, table, q_weight, k_weight, eps, interleaved)
         if got is not None:
             return _got(got)
+    _no_tangent(gq, gk, q, k, table, q_weight, k_weight, dq, dk)
     n, hq, D = q.shape
     hk = k.shape[1]
     qs, ks = _heads(q, n, hq, D, q.dtype), _heads(k, n, hk, D, q.dtype)

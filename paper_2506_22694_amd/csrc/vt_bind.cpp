@@ -222,9 +222,9 @@ decltype(&vt_kv_cache_read) g_read = nullptr;
 decltype(&vt_paged_attention) g_attend = nullptr;
 
 bool given(PyObject *o) { return o != Py_None; }
-// A gradient is asked for of the tensor: autograd's business, or a refusal
+// A gradient is asked for of the tensor, or it has a tangent: autograd's business, or a refusal
 const at::Tensor &plain(const at::Tensor &t) {
-    if (c10::GradMode::is_enabled() && t.requires_grad()) throw NotPlain();
+    if ((c10::GradMode::is_enabled() && t.requires_grad()) || t._fw_grad(0).defined()) throw NotPlain();
     return t;
 }
 

@@ -1,6 +1,7 @@
 """What the attention's calls do where a gradient is asked for: qk_norm_rope has one, the cache and the attention over it refuse."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import paper_2506_22694_amd as vt
 
@@ -45,3 +46,24 @@ def test_no_gradient_is_lost_on_the_device():
             call()
     torch.cuda.synchronize()
     assert x.eq(1).all() and leaf.grad is None
+
+
+@pytest.mark.parametrize("device", ["cpu", pytest.param("cuda", marks=pytest.mark.gpu)])
+def test_dual_tensors_are_refused(device):
+    x, w, table = torch.ones(2, 2, 64, device=device), torch.ones(64, device=device), torch.ones(8, 64, device=device)
+    slots, pages, lengths = torch.arange(2, device=device), torch.zeros(2, 1, dtype=torch.int32, device=device), torch.ones(2, dtype=torch.int32, device=device)
+    cache = ws = None
+    if device == "cuda":
+        cache, ws = vt.KVCache(1, 16, 2, 64), vt.AttentionWorkspace(2, 2, 2, 64, 2, 1, 16, device)
+    with forward_ad.dual_level():
+        dx, dw, dt = (forward_ad.make_dual(t, torch.ones_like(t)) for t in (x, w, table))
+        calls = [lambda: vt.qk_norm_rope(dx, x), lambda: vt.qk_norm_rope(x, dx), lambda: vt.qk_norm_rope(x, x, None, None, dw, w), lambda: vt.qk_norm_rope(x, x, None, None, w, dw),
+                 lambda: vt.qk_norm_rope(x, x, slots, dt), lambda: vt.qk_norm_rope_backward(dx, x, x, x, None, None, w, w),
+                 lambda: vt.qk_norm_rope_backward(x, x, x, dx, None, None, w, w), lambda: vt.qkv_to_cache(dx, x, x, cache, slots), lambda: vt.qkv_to_cache(x, x, dx, cache, slots),
+                 lambda: vt.kv_cache_write(cache, dx, x, slots), lambda: vt.paged_attention(dx, cache, pages, lengths, ws=ws)]
+        for call in calls:
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(ValueError, match="no tangent"):
+                    call()
+        if device == "cuda":      # others' tangents are nobody's business
+            vt.paged_attention(x, cache, pages, lengths, ws=ws)
