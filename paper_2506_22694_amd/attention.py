@@ -97,6 +97,12 @@ def _norm_arguments(q, n, D, positions, table, q_weight, k_weight, eps, interlea
 
 
 # --------------------------------------------------------------------------- norm and rotation
+def _own_rows(g: torch.Tensor) -> torch.Tensor:
+    """A gradient as the library takes it: those of sums and broadcasts have no rows of their own, pieces of one may begin anywhere."""
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 class _QkNormRope(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, positions, table, q_weight, k_weight, eps, interleaved):
@@ -108,9 +114,7 @@ class _QkNormRope(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, gq, gk):
         q, k, positions, table, q_weight, k_weight = ctx.saved_tensors
-        # (gradients of sums and broadcasts are views without rows of their own)
-        dq, dk, dqw, dkw = qk_norm_rope_backward(gq.contiguous(), gk.contiguous(), q, k, positions, table, q_weight, k_weight, ctx.eps,
-                                                 ctx.interleaved)
+        dq, dk, dqw, dkw = qk_norm_rope_backward(_own_rows(gq), _own_rows(gk), q, k, positions, table, q_weight, k_weight, ctx.eps, ctx.interleaved)
         if dqw is not None:
             dqw, dkw = dqw.view_as(q_weight).to(q_weight.dtype), dkw.view_as(k_weight).to(k_weight.dtype)
         return dq, dk, None, None, dqw, dkw, None, None

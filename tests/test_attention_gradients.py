@@ -67,3 +67,22 @@ def test_dual_tensors_are_refused(device):
                     call()
         if device == "cuda":      # others' tangents are nobody's business
             vt.paged_attention(x, cache, pages, lengths, ws=ws)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("ahead", [1, 3, 8])
+def test_gradients_that_begin_anywhere(dtype, ahead):
+    """A piece of a concatenation's gradient is contiguous, and at no multiple of 16 bytes."""
+    g = torch.Generator(device="cuda").manual_seed(ahead)
+
+    def randn(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(dtype)
+    q, k, wq, wk = randn(5, 4, 64).requires_grad_(), randn(5, 2, 64).requires_grad_(), randn(64).requires_grad_(), randn(64).requires_grad_()
+    y, z = vt.qk_norm_rope(q, k, None, None, wq, wk)
+    given = randn(ahead + y.numel() + z.numel() + ahead)
+    torch.cat([randn(ahead), y.flatten(), randn(ahead), z.flatten()]).backward(given)
+    gy, gz = given[ahead:ahead + y.numel()].clone().view_as(y), given[2 * ahead + y.numel():].clone().view_as(z)
+    want = vt.qk_norm_rope_backward(gy, gz, q.detach(), k.detach(), None, None, wq.detach(), wk.detach())
+    for x, w in zip((q, k, wq, wk), want):
+        assert torch.equal(x.grad, w.to(dtype))
