@@ -40,55 +40,75 @@ class Drafter:
         """q, k, v [n, heads, head_dim] of rows x: views of one product."""
         return torch.split((x @ self.qkv).unflatten(1, (-1, self.head_dim)), [self.q_heads, self.kv_heads, self.kv_heads], dim=1)
 
-    def layer(self, tokens, cache, slots, positions, page_table, lengths, tail_mask=None):
+    def layer(self, tokens, cache, slots, positions, page_table, lengths, ws, max_length, row_start=None, tail_mask=None):
         """Hidden rows of new tokens of one request, whose keys and values go to `slots`."""
         x = self.embedding[tokens]
         q, k, v = self.project(x)
         q = vt.qkv_to_cache(q, k, v, cache, slots, positions, self.rope, self.q_norm, self.k_norm)
-        rows = torch.tensor([0, tokens.numel()], dtype=torch.int32, device=x.device)
-        a = vt.paged_attention(q, cache, page_table, lengths, row_start=rows, max_rows=tokens.numel(), tail_mask=tail_mask)
+        a = vt.paged_attention(q, cache, page_table, lengths, row_start=row_start, max_rows=None if row_start is None else tokens.numel(),
+                               tail_mask=tail_mask, max_length=max_length, ws=ws)
         return x + a.flatten(1) @ self.out
 
 
-def draft_round(drafter, prompt, cache, page_table, depth=3, width=8, keep=32):
+class Memory:
+    """What a program keeps from one round to the next: the calls' workspaces and a tree's memory."""
+
+    def __init__(self, drafter, most_tokens, depth=3, width=8, keep=32, device="cuda"):
+        k, d = drafter.head.shape
+        self.depth, self.width, self.keep = depth, width, min(keep, depth * width)
+        self.attend = vt.AttentionWorkspace(width, drafter.q_heads, drafter.kv_heads, drafter.head_dim, 1, width, most_tokens + depth * width, device)
+        self.step = vt.StepWorkspace(width, k, d, width, device)
+        self.rows = torch.arange(0, width + 1, width, dtype=torch.int32, device=device)      # a level's rows are one request's
+        self.ids = torch.empty(width, width, dtype=torch.int32, device=device)
+        self.logp = torch.empty(width, width, device=device)
+
+    def tree(self, device):
+        """Memory of one tree: parents (rows of the level before), tokens, cumulative log-probabilities, a row to each level; kept nodes."""
+        shape = (self.depth, self.width)
+        return (torch.empty(shape, dtype=torch.int32, device=device), torch.empty(shape, dtype=torch.int32, device=device),
+                torch.empty(shape, device=device), torch.empty(self.keep, dtype=torch.int32, device=device))
+
+
+def draft_round(drafter, prompt, cache, page_table, depth=3, width=8, keep=32, memory=None):
     """Drafts a tree behind `prompt` (token ids of one request).  Returns a dict of the tree's nodes in the order they were
-    drafted: token, parent (-1: the prompt), depth, cumulative log-probability, hidden row each was drafted from; and `kept`."""
+    drafted: token, parent (-1: the prompt), depth, cumulative log-probability, hidden row each was drafted from; and `kept`.
+    `memory`: one that is kept, whose depth, width and keep hold."""
     dev, n = prompt.device, prompt.numel()
+    memory = memory or Memory(drafter, n, depth, width, keep, dev)
+    depth, width = memory.depth, memory.width
+    parents, tokens, cums, kept = memory.tree(dev)
     one = torch.zeros((), dtype=torch.int64, device=dev)
 
     def slots_of(first, count):
         return cache.slots(page_table, one.expand(count), torch.arange(first, first + count, device=dev))
-
-    def length(tokens):
-        return torch.tensor([tokens], dtype=torch.int32, device=dev)
+    lengths = torch.arange(n, n + depth * width, width, dtype=torch.int32, device=dev)      # cached tokens, with those of a level
     # the prompt but its newest token: for its keys and values only
     if n > 1:
         q, k, v = drafter.project(drafter.embedding[prompt[:-1]])
         vt.qkv_to_cache(q, k, v, cache, slots_of(0, n - 1), torch.arange(n - 1, device=dev), drafter.rope, drafter.q_norm, drafter.k_norm)
-    hidden = drafter.layer(prompt[-1:], cache, slots_of(n - 1, 1), torch.tensor([n - 1], device=dev), page_table, length(n))
+    hidden = drafter.layer(prompt[-1:], cache, slots_of(n - 1, 1), torch.arange(n - 1, n, device=dev), page_table, lengths[:1], memory.attend, n)
 
-    tree = {"token": [], "parent": [], "depth": [], "cum": [], "hidden": []}
+    drafted_from, frontiers = [], []
     frontier = torch.full((1,), -1, dtype=torch.int64, device=dev)      # node numbers of the rows of `hidden`
     cum = torch.zeros(1, device=dev)
     seen = torch.zeros(1, dtype=torch.int64, device=dev)                # of each frontier node: itself and its ancestors, a bit each
     for level in range(depth):
-        parent, token, cum, _, _ = vt.draft_tree_level(hidden, drafter.head, drafter.map, width, cum, width)
-        parent, drafted = parent.long(), level * width
-        tree["token"].append(token)
-        tree["parent"].append(frontier[parent])
-        tree["depth"].append(torch.full_like(token, level))
-        tree["cum"].append(cum)
+        rows = hidden.shape[0]
+        vt.draft_tree_level(hidden, drafter.head, drafter.map, width, cum, width, ws=memory.step, out=(parents[level], tokens[level], cums[level]),
+                            out_ids=memory.ids[:rows], out_logp=memory.logp[:rows])
+        parent, cum, drafted = parents[level].long(), cums[level], level * width
+        drafted_from.append(hidden[parent])
+        frontiers.append(frontier[parent])
         frontier = torch.arange(drafted, drafted + width, device=dev)
         seen = seen[parent] | (1 << frontier)
-        tree["hidden"].append(hidden[parent])
         if level + 1 < depth:
             nodes = drafted + width
             mask = (seen << (64 - nodes)) | ((1 << (64 - nodes)) - 1)      # bit j: token n + nodes - 64 + j
-            hidden = drafter.layer(token, cache, slots_of(n + drafted, width), torch.full((width,), n + level, device=dev), page_table,
-                                   length(n + nodes), mask)
-    tree = {name: torch.cat(parts) for name, parts in tree.items()}
-    tree["kept"] = vt.tree_rerank(tree["cum"], min(keep, depth * width))
-    return tree
+            hidden = drafter.layer(tokens[level], cache, slots_of(n + drafted, width), torch.full((width,), n + level, device=dev), page_table,
+                                   lengths[level + 1:level + 2], memory.attend, n + nodes, memory.rows, mask)
+    vt.tree_rerank(cums.flatten(), memory.keep, out=kept)
+    return {"token": tokens.flatten(), "parent": torch.cat(frontiers), "depth": torch.arange(depth, dtype=torch.int32, device=dev).repeat_interleave(width),
+            "cum": cums.flatten(), "hidden": torch.cat(drafted_from), "kept": kept}
 
 
 def main():

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2506_22694_amd as vt
+from paper_2506_22694_amd import binding
 from test_gpu_draft_round import _example
 
 pytestmark = pytest.mark.gpu
@@ -84,3 +85,31 @@ def test_the_attention_of_every_node(held, n, page):
             first = parent[i] // width * width
             other = n + (parent[i] + 1 if parent[i] + 1 < first + width else first)
             assert _rms(got - x - share([other] + seen[1:])) > 2 * bound and _rms(got - x - share(seen[1:])) > 2 * bound, i
+
+
+def test_a_round_takes_the_native_way_and_copies_nothing_from_the_host(monkeypatch):
+    example = _example()
+    drafter = example.Drafter(d=512, q_heads=4, kv_heads=2, head_dim=64, vocabulary=4000, trimmed=1000)
+    cache, table = vt.KVCache(4, 64, 2, 64), torch.arange(4, dtype=torch.int32, device="cuda")[None].contiguous()
+    prompt = torch.arange(100, device="cuda")
+    memory = example.Memory(drafter, 200, 3, 8, 16)
+    want = example.draft_round(drafter, prompt, cache, table, memory=memory)
+    asked, native = [], binding._bind
+
+    class Spy:
+        def __getattr__(self, name):
+            def call(*a):
+                got = getattr(native, name)(*a)
+                asked.append((name, got is not None and not (type(got) is int and got < 0)))
+                return got
+            return call
+    monkeypatch.setattr(binding, "_bind", Spy())
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        got = example.draft_round(drafter, prompt, cache, table, memory=memory)
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    names = [name for name, _ in asked]
+    assert all(done for _, done in asked) and [names.count(x) for x in ("to_cache", "attend", "level", "rerank")] == [4, 3, 3, 1]
+    for key in want:
+        assert torch.equal(got[key], want[key]), key
