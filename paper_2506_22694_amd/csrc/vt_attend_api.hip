@@ -69,6 +69,8 @@ struct Split {
 // Shares that all requests' tokens are cut into: two workgroups' on each of the 256 CUs, all there at a time, the one reading while the other
 // begins or ends a request (48 ragged requests in 8 bits 104 us, with one on each CU 107, with four 106).  One request has one beginning,
 // and the workgroups of a CU take each other's time: 16384 tokens 17.2 us with one on each CU, 18.5 with two; 131001 tokens 88.0 and 88.8.
+// (Levels of a few short requests have no more steps than places: there it is one step to a workgroup and one tile to a wave, whose loads have
+// nothing to hide behind.  Longer shares were not measured on them.)
 constexpr int64_t kAttendWorkgroups = 512, kAttendWorkgroupsOfOne = 256;
 // Up to here a workgroup takes a request whole, without the second launch: 300 tokens of one request 6.6 us whole, 7.9 in shares, 512 tokens
 // 8.9 and 8.0.  Where there are many requests the workgroups are enough: of two requests' worth of tokens for each workgroup and no more

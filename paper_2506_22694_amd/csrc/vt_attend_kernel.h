@@ -24,7 +24,7 @@
 // 8 bits 61 instead of 65, 16 nodes of 64 heads of 64 values 71 instead of 81.)
 //
 // 131001 tokens of one request, 8 kv heads of 128 values in bf16, 4 query heads each: 537 MB in 80 us, 6.7 TB/s, where a plain read of as much
-// takes 79; 151 vector and 16 matrix instructions a tile (8 bits: 268 and 16; 48 ragged requests 541 MB in 94 us, 5.8 TB/s).
+// takes 79; 224 vector and 32 matrix instructions a tile (8 bits: 317 and 32; 48 ragged requests 541 MB in 95 us, 5.7 TB/s).
 #pragma once
 #include "vt_values.h"
 
@@ -154,8 +154,8 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     return s;
 }
 
-// Waves on a SIMD that the registers are cut to: as many as fit without scratch memory (fp32 rows of 256 values keep 24 bytes of it, outside
-// the loop over tiles).  Two at least, so that there are 256 vector
+// Waves on a SIMD that the registers are cut to: as many as fit without scratch memory (fp32 rows of 256 values over a 16-bit cache keep
+// 16 bytes of it, and read 8 of those, the tail mask, in the tiles that it applies to).  Two at least, so that there are 256 vector
 // registers and no accumulation registers: copies out of those have come ahead of the matrix instructions' results here (a branch right
 // behind the last product: clang 20 leaves out the wait states on its way), which the build checks there are none of.
 template <int DP, bool FP8, int NT, bool F32Q>
