@@ -1,8 +1,9 @@
 /*
  * vocabtrim_attention.h -- the attention of a drafter's layer, the step ahead of
  * the trimmed head: norms of queries and keys with the position rotation (and
- * their gradients), a paged key-value cache in 16 or 8 bits, and the attention
- * of a draft step's new tokens over it.
+ * their gradients), a paged key-value cache in 16, 8 or 4 bits, and the attention
+ * of a draft step's new tokens over it, with a sliding window and sinks where the
+ * layer has them.
  *
  * The general conventions of vocabtrim.h hold: device pointers of the caller's,
  * nothing allocated, kept or synchronised, work enqueued on `stream`, errors
@@ -76,13 +77,17 @@ size_t vt_qk_norm_rope_backward_ws_bytes(int64_t n, int32_t head_dim);
 /* ------------------------------------------------------------------------
  * A paged key-value cache: caller's memory, described by this struct (HOST).
  *
- *   k, v              [pages, heads, page_size, head_dim] of type VT_BF16 or VT_E4M3
+ *   k, v              [pages, heads, page_size, head_dim] of type VT_BF16, VT_E4M3 or
+ *                     VT_E2M1 (4 bits each: value 2 i of a row in the lower half of its
+ *                     byte i, 2 i + 1 in the upper)
  *   k_scale, v_scale  [pages, heads, page_size] exponents of the scales, VT_E4M3
  *                     only (else NULL): code c stands for c * 2^(scale - 127).  (255 has
  *                     no place in fp32 but for the least codes: what reads or sees such
  *                     a token may get infinities and NaN.)
+ *                     VT_E2M1: [pages, heads, head_dim / 32, page_size], scales of the
+ *                     values 32 j .. 32 j + 31 of every token (255: they are NaN)
  *   page_size         a power of two, 16 .. 65536
- *   head_dim          a multiple of 16, <= VT_MAX_HEAD_DIM
+ *   head_dim          a multiple of 16 (VT_E2M1: of 32), <= VT_MAX_HEAD_DIM
  *
  * A head's tokens of a page are one stretch of memory.  A SLOT is
  * page * page_size + place.  An e4m3 row has the smallest scale 2^e, e >= -126,
@@ -90,6 +95,11 @@ size_t vt_qk_norm_rope_backward_ws_bytes(int64_t n, int32_t head_dim);
  * nearest even, at most +-448 * 2^e (240 * 2^120, the scale of the largest fp32
  * values: no held value is infinite), infinities to those; NaN is held as NaN.  A power of two
  * makes the scaling exact and every held value exact in bf16.
+ *
+ * A code of 4 bits is a sign and the number of a magnitude among 0, 0.5, 1, 1.5, 2, 3, 4, 6.  32
+ * values have the smallest scale 2^e, e >= -126, with max |x| <= 6 * 2^e over the finite ones; a
+ * value is rounded to the nearest (of two as near, the even number), at most +-6 * 2^e (3 * 2^126),
+ * infinities to those; a group with NaN in it is NaN.
  * ---------------------------------------------------------------------- */
 typedef struct {
     void *k, *v;
@@ -100,7 +110,8 @@ typedef struct {
 } vt_kv_cache;
 
 /* vt_qk_norm_rope on q and k, with k and v written into the cache in the same
- * launch (k rounded once, from fp32 to what the cache holds).
+ * launch (k rounded once, from fp32 to what the cache holds; to 4 bits from 64, so that a code is
+ * the formula's also where fp32's last bits would decide between two).
  *   q        NULL with q_heads == 0 writes the cache only
  *   k, v     [n, cache->heads, cache->head_dim]
  *   slots    [n] int32 or int64 (slot_type): where each row's k and v go.  A slot
@@ -156,9 +167,32 @@ int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int
                        const int32_t *row_start, int32_t max_rows, const uint64_t *tail_mask, int64_t max_length,
                        float scale, void *out, int64_t out_stride, float *out_lse, void *ws, size_t ws_bytes,
                        void *stream);
-/* Enough for every call of up to these sizes (kv_heads and head_dim as they are); 0 also for arguments out of range. */
+/* Enough for every call of up to these sizes, with a window or without (kv_heads and head_dim as they are); 0 also for arguments out of range. */
 size_t vt_paged_attention_ws_bytes(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t n_requests,
                                    int32_t max_rows, int64_t max_length);
+
+/* The same on a layer with a sliding window and sinks (first tokens that stay visible).  Of the
+ * tokens that a row sees as above, a row at position p sees those with
+ *
+ *   t > p - window   or   t < sinks
+ *
+ * and a request's other tokens are not read, their pages' entries not used (but for the pages that hold
+ * the up to 64 tokens ahead of a window): the time follows the window, not the lengths.
+ *
+ *   tail_mask     NULL: a row sees no token behind itself either, t <= p.  (A prompt's chunk, its keys
+ *                 in the cache: max_rows is the longest chunk.)
+ *   positions     [n] int32 or int64 (pos_type), with a tail mask only (the nodes of a tree: the
+ *                 prompt's length plus their depth); one below lengths[b] - 64 counts as that.
+ *                 NULL: a request's R rows are its last tokens, p = lengths[b] - R + (0 .. R - 1)
+ *                 (R: at most max_rows)
+ *   window        1 .. 2^30; from max_length on: every token up to the row's own
+ *   sinks         0 .. 2^30
+ * Workspace as for vt_paged_attention with the same sizes. */
+int vt_paged_attention_window(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache,
+                              const int32_t *page_table, int32_t table_pages, const int32_t *lengths, int32_t n_requests,
+                              const int32_t *row_start, int32_t max_rows, const uint64_t *tail_mask, const void *positions,
+                              int pos_type, int64_t window, int64_t sinks, int64_t max_length, float scale, void *out,
+                              int64_t out_stride, float *out_lse, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

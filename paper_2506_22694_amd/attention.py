@@ -1,7 +1,7 @@
 """The attention of a drafter's layer: binding over include/vocabtrim_attention.h.
 
-Norms of queries and keys with the position rotation (and their gradients), a paged key-value cache in 16 or 8 bits,
-and the attention of a draft step's new tokens over it.  As in binding.py, tensors supply memory and the current
+Norms of queries and keys with the position rotation (and their gradients), a paged key-value cache in 16, 8 or 4 bits,
+and the attention of new tokens over it, with a sliding window and sinks where the layer has them.  As in binding.py, tensors supply memory and the current
 stream; every step runs in the library's kernels, and what it refuses is raised.
 
 Tensors of heads are [n, heads, head_dim]: rows may lie apart (views of one projection's output), a row's heads and
@@ -17,7 +17,8 @@ from torch.autograd import forward_ad
 from . import binding
 from .binding import VT_I32, VT_I64, _check, _dtype_code, _ptr, _require_cuda, _scratch, _stream, load_library
 
-VT_E4M3 = 2
+VT_E4M3, VT_E2M1 = 2, 4
+GROUP = 32      # values of a 4-bit row that share a scale
 VT_ROPE_HALVES, VT_ROPE_NEIGHBOURS = 0, 1
 
 
@@ -199,15 +200,22 @@ class _CacheStruct(ctypes.Structure):
 
 class KVCache:
     """A paged key-value cache on the device: k and v [pages, heads, page_size, head_dim], bfloat16 or float8_e4m3fn with the
-    exponents of its scales [pages, heads, page_size] (uint8).  Its memory needs no initialisation.  A slot is
-    page * page_size + place."""
+    exponents of its scales [pages, heads, page_size] (uint8).  In 4 bits, float4_e2m1fn_x2 (two values to a byte, the first in
+    its lower half), k and v are [pages, heads, page_size, head_dim / 2], head_dim a multiple of 32, and the scales' exponents
+    [pages, heads, head_dim / 32, page_size].  Its memory needs no initialisation.  A slot is page * page_size + place."""
 
     def __init__(self, pages: int, page_size: int, heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        four = dtype == torch.float4_e2m1fn_x2
+        if four and head_dim % GROUP:
+            raise ValueError("head_dim of a 4-bit cache must be a multiple of 32")
+
         def held():
-            return torch.empty((pages, heads, page_size, head_dim), dtype=dtype, device=device)
+            return torch.empty((pages, heads, page_size, head_dim // 2 if four else head_dim), dtype=dtype, device=device)
 
         def scale():
-            return torch.empty((pages, heads, page_size), dtype=torch.uint8, device=device) if dtype == torch.float8_e4m3fn else None
+            if dtype == torch.bfloat16:
+                return None
+            return torch.empty((pages, heads, head_dim // GROUP, page_size) if four else (pages, heads, page_size), dtype=torch.uint8, device=device)
 
         self._set(held(), held(), scale(), scale())
 
@@ -219,19 +227,24 @@ class KVCache:
         return cache
 
     def _set(self, k, v, k_scale, v_scale):
-        coded = k.dtype == torch.float8_e4m3fn
-        if not coded and k.dtype != torch.bfloat16:
+        held = {torch.bfloat16: 1, torch.float8_e4m3fn: VT_E4M3, torch.float4_e2m1fn_x2: VT_E2M1}.get(k.dtype)
+        if held is None:
             raise TypeError(f"unsupported element type of a cache {k.dtype}")
         if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v must be [pages, heads, page_size, head_dim] of one type")
+        pages, heads, page_size, head_dim = k.shape
+        scales = (pages, heads, page_size)
+        if held == VT_E2M1:
+            head_dim *= 2
+            scales = (pages, heads, head_dim // GROUP, page_size)
         for s in (k_scale, v_scale):
-            if (s is not None) != coded or (coded and (s.shape != k.shape[:3] or s.dtype != torch.uint8)):
-                raise ValueError("k_scale and v_scale must be uint8 [pages, heads, page_size], of an 8-bit cache only")
+            if (s is not None) != (held != 1) or (s is not None and (tuple(s.shape) != scales or s.dtype != torch.uint8)):
+                raise ValueError("k_scale and v_scale must be uint8 [pages, heads, page_size] of an 8-bit cache, [pages, heads, head_dim / 32, page_size] of a "
+                                 "4-bit one, and are not of a 16-bit one")
         _no_gradient(k, v)
         _require_cuda(k, v, k_scale, v_scale)
         self._tensors = (k, v, k_scale, v_scale)
-        pages, heads, page_size, head_dim = k.shape
-        self._struct = _CacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), VT_E4M3 if coded else 1, pages, heads, page_size, head_dim)
+        self._struct = _CacheStruct(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), held, pages, heads, page_size, head_dim)
         self._address = ctypes.addressof(self._struct)
 
     k = property(lambda self: self._tensors[0])
@@ -324,18 +337,24 @@ class AttentionWorkspace:
 def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lengths: torch.Tensor,
                     row_start: torch.Tensor | None = None, max_rows: int | None = None, tail_mask: torch.Tensor | None = None,
                     max_length: int | None = None, scale: float | None = None, ws: AttentionWorkspace | None = None,
-                    out: torch.Tensor | None = None, return_lse: bool = False, out_lse: torch.Tensor | None = None):
+                    out: torch.Tensor | None = None, return_lse: bool = False, out_lse: torch.Tensor | None = None,
+                    window: int | None = None, sinks: int = 0, positions: torch.Tensor | None = None):
     """Attention of q [n, q_heads, head_dim] over the cached tokens of their requests: out like q [, lse float32 [n, q_heads]].
 
     page_table int32 [requests, pages of each], lengths int32 [requests].  Row i is request i's, or rows
     row_start[b] .. row_start[b + 1] - 1 are request b's, at most max_rows (other rows are not computed).  tail_mask (int64 [n], its bits): which of
     the last 64 tokens a row sees, bit j being token length - 64 + j.  scale: of the scores (head_dim^-1/2).
     max_length: no request is longer (the page table's width, where it isn't given; near the longest is fastest).
+
+    window, sinks: the row at position p sees no tokens but t > p - window and t < sinks, and only those of a request are read that
+    some row sees.  A request's rows are its last tokens and, without a tail mask, see none behind themselves: a prompt's chunk
+    whose keys are cached.  With a tail mask the nodes of a tree may have `positions` (int32 or int64 [n]; the prompt's length plus
+    their depth), which count from the first of the last 64 tokens on.  A window of max_length and more: all tokens up to the row's own.
     A q that requires a gradient is refused: there is none."""
     L = load_library()
     if binding._bind is not None and type(ws) is AttentionWorkspace and type(cache) is KVCache:
         got = binding._bind.attend(q, cache._address, page_table, lengths, row_start, max_rows, tail_mask, max_length, scale, ws.buf, out, return_lse,
-                                   out_lse)
+                                   out_lse, window, sinks, positions)
         if got is not None:
             return _got(got)
     _no_gradient(q, out, out_lse)
@@ -355,6 +374,11 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
         raise ValueError("row_start must be int32 [requests + 1]")
     if tail_mask is not None and (tail_mask.dtype not in (torch.int64, torch.uint64) or tail_mask.numel() != n):
         raise ValueError("tail_mask must be int64 [n]")
+    if window is None and (sinks != 0 or positions is not None):
+        raise ValueError("sinks and positions are a window's")
+    if positions is not None and tail_mask is None:
+        raise ValueError("positions go with a tail mask: without one a request's rows are its last tokens")
+    pos_type = VT_I32 if positions is None else _index(positions, n, "positions")
     if max_length is None:
         max_length = pages * cache.page_size
     if scale is None:
@@ -369,7 +393,11 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
         out_lse = torch.empty((n, hq), dtype=torch.float32, device=dev)
     if ws is None:
         ws = AttentionWorkspace(n, hq, cache.heads, D, requests, max_rows, max_length, dev)
-    _check(L.vt_paged_attention(_ptr(q), _heads(q, n, hq, D, q.dtype), _dtype_code(q), n, hq, cache._address, _ptr(page_table), pages,
-                                _ptr(lengths), requests, _ptr(row_start), max_rows, _ptr(tail_mask), max_length, scale, _ptr(out),
-                                _heads(out, n, hq, D, q.dtype), _ptr(out_lse), _ptr(ws.buf), ws.nbytes, _stream(dev)))
+    what = (_ptr(q), _heads(q, n, hq, D, q.dtype), _dtype_code(q), n, hq, cache._address, _ptr(page_table), pages, _ptr(lengths), requests, _ptr(row_start),
+            max_rows, _ptr(tail_mask))
+    how = (max_length, scale, _ptr(out), _heads(out, n, hq, D, q.dtype), _ptr(out_lse), _ptr(ws.buf), ws.nbytes, _stream(dev))
+    if window is None:
+        _check(L.vt_paged_attention(*what, *how))
+    else:
+        _check(L.vt_paged_attention_window(*what, _ptr(positions), pos_type, window, sinks, *how))
     return (out, out_lse) if return_lse else out

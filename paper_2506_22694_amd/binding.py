@@ -31,7 +31,7 @@ EXPORTS = (
     "vt_tree_expand", "vt_tree_rerank", "vt_draft_tree_level", "vt_stream_read_reference",
     "vt_build_trimmed_heads", "vt_draft_head_step_multi", "vt_draft_head_step_multi_ws_bytes",
     "vt_qk_norm_rope", "vt_qk_norm_rope_backward", "vt_qk_norm_rope_backward_ws_bytes",
-    "vt_qkv_to_cache", "vt_kv_cache_read", "vt_paged_attention", "vt_paged_attention_ws_bytes",
+    "vt_qkv_to_cache", "vt_kv_cache_read", "vt_paged_attention", "vt_paged_attention_window", "vt_paged_attention_ws_bytes",
 )
 VT_MAX_HEADS, VT_MULTI_MAX_ROWS = 16, 256
 VT_TREE_MAX_CANDIDATES, VT_TREE_MAX_KEEP = 16384, 1024
@@ -108,6 +108,8 @@ def load_library() -> ctypes.CDLL:
     L.vt_kv_cache_read.restype = ci
     L.vt_paged_attention.argtypes = [vp, i64, ci, i64, i32, vp, vp, i32, vp, i32, vp, i32, vp, i64, f32, vp, i64, vp, vp, sz, vp]
     L.vt_paged_attention.restype = ci
+    L.vt_paged_attention_window.argtypes = [vp, i64, ci, i64, i32, vp, vp, i32, vp, i32, vp, i32, vp, vp, ci, i64, i64, i64, f32, vp, i64, vp, vp, sz, vp]
+    L.vt_paged_attention_window.restype = ci
     L.vt_paged_attention_ws_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i64]
     L.vt_paged_attention_ws_bytes.restype = sz
     _connect(L)
@@ -136,7 +138,7 @@ def _connect(L) -> None:
     _vt_bind.connect(_raw_stream, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.vt_draft_head_step, L.vt_draft_head_step_static, L.vt_draft_tree_level, L.vt_tree_rerank, L.vt_count_tokens,
         L.vt_qk_norm_rope, L.vt_qk_norm_rope_backward, L.vt_qk_norm_rope_backward_ws_bytes, L.vt_qkv_to_cache, L.vt_kv_cache_read,
-        L.vt_paged_attention)))
+        L.vt_paged_attention, L.vt_paged_attention_window)))
     _bind = _vt_bind
 
 

@@ -116,7 +116,11 @@ int attend_row_tiles(int rows, int D, bool f32) {
 
 hipError_t launch_attend(const AttendArgs &a, bool f32, hipStream_t st) {
     const int D = a.cache.D, tiles = a.row_tiles;
-    hipError_t e = D <= 64 ? launch_attend_d64(a, tiles, f32, st) : D <= 128 ? launch_attend_d128(a, tiles, f32, st) : launch_attend_d256(a, tiles, f32, st);
+    hipError_t e;
+    if (a.window > 0)
+        e = D <= 64 ? launch_attend_window_d64(a, tiles, f32, st) : D <= 128 ? launch_attend_window_d128(a, tiles, f32, st) : launch_attend_window_d256(a, tiles, f32, st);
+    else
+        e = D <= 64 ? launch_attend_d64(a, tiles, f32, st) : D <= 128 ? launch_attend_d128(a, tiles, f32, st) : launch_attend_d256(a, tiles, f32, st);
     if (e != hipSuccess || a.whole) return e;
     if (D <= 64) run_join<16>(a, f32, st);
     else if (D <= 128) run_join<32>(a, f32, st);

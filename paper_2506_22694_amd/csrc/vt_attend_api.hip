@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "vt_attn.h"
+#include "vt_cells.h"
 
 namespace {
 
@@ -45,18 +46,19 @@ int norm_status(int type, int64_t n, int q_heads, int k_heads, int D, const void
 
 int cache_status(const vt_kv_cache *c) {
     if (c == nullptr) return VT_ERR_NULL;
-    if (c->type != VT_BF16 && c->type != VT_E4M3) return VT_ERR_DTYPE;
+    if (c->type != VT_BF16 && c->type != VT_E4M3 && c->type != VT_E2M1) return VT_ERR_DTYPE;
     if (c->pages < 1 || c->pages > kMaxRows || c->heads < 1 || c->heads > VT_MAX_ATTENTION_HEADS || c->head_dim < 16 || c->head_dim > VT_MAX_HEAD_DIM ||
         c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0)
         return VT_ERR_SHAPE;
     if (c->k == nullptr || c->v == nullptr) return VT_ERR_NULL;
-    if (c->type == VT_E4M3 && (c->k_scale == nullptr || c->v_scale == nullptr)) return VT_ERR_NULL;
-    if (c->head_dim % 16 != 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return VT_ERR_ALIGN;
-    return c->type != VT_E4M3 || (aligned(c->k_scale, 4) && aligned(c->v_scale, 4)) ? VT_OK : VT_ERR_ALIGN;
+    const bool coded = c->type != VT_BF16;
+    if (coded && (c->k_scale == nullptr || c->v_scale == nullptr)) return VT_ERR_NULL;
+    if (c->head_dim % (c->type == VT_E2M1 ? vt::kScaleGroup : 16) != 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return VT_ERR_ALIGN;
+    return !coded || (aligned(c->k_scale, 4) && aligned(c->v_scale, 4)) ? VT_OK : VT_ERR_ALIGN;
 }
 vt::CacheArgs cache_args(const vt_kv_cache &c) {
-    const bool coded = c.type == VT_E4M3;
-    return {c.k, c.v, coded ? c.k_scale : nullptr, coded ? c.v_scale : nullptr, c.pages, c.heads, __builtin_ctz((unsigned)c.page_size), c.head_dim};
+    const bool coded = c.type != VT_BF16;
+    return {c.k, c.v, coded ? c.k_scale : nullptr, coded ? c.v_scale : nullptr, c.pages, c.heads, __builtin_ctz((unsigned)c.page_size), c.head_dim, c.type == VT_E2M1};
 }
 
 // How attention is cut up: blocks of a kv head's query rows, and shares of all requests' tokens.
@@ -109,6 +111,52 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     s.entries = (size_t)units * places * 2 * per;
     s.bytes = s.entries * entry + requests * sizeof(int4);
     return s;
+}
+
+// Both calls' checks and launch; a window of 0: none.
+int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache, const int32_t *page_table,
+              int32_t table_pages, const int32_t *lengths, int32_t n_requests, const int32_t *row_start, int32_t max_rows, const uint64_t *tail_mask,
+              int64_t window, int64_t sinks, const void *positions, int pos_type, int64_t max_length, float scale, void *out, int64_t out_stride,
+              float *out_lse, void *ws, size_t ws_bytes, void *stream) {
+    int s = cache_status(cache);
+    if (s != VT_OK) return s;
+    if (!element(type)) return VT_ERR_DTYPE;
+    const bool f32 = type == VT_F32;
+    // tokens of a request that any of its rows may see, counted in whole 16 at either end of the gap
+    int64_t seen = max_length;
+    if (window > 0) {
+        const int64_t most = sinks + 15 + window + 15 + (positions != nullptr ? vt::kTail : max_rows);
+        seen = most < max_length ? most : max_length;
+        // (what the workspace's size is asked with)
+        if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32).ok) return VT_ERR_SHAPE;
+    }
+    const Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32);
+    if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
+    if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
+    if (n == 0 || n_requests == 0) return VT_OK;
+    if (page_table == nullptr || lengths == nullptr) return VT_ERR_NULL;
+    if ((s = heads_status(q, q_stride, q_heads, cache->head_dim)) != VT_OK) return s;
+    if ((s = heads_status(out, out_stride, q_heads, cache->head_dim)) != VT_OK) return s;
+    if (!aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(row_start, 4) || !aligned(tail_mask, 8)) return VT_ERR_ALIGN;
+    if (split.bytes > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < split.bytes)) return VT_ERR_WORKSPACE;
+    if (!aligned(out_lse, 4)) return VT_ERR_ALIGN;
+    vt::AttendArgs a{};
+    a.q = q, a.q_stride = q_stride, a.n = (int)n, a.hq = q_heads, a.G = q_heads / cache->heads;
+    a.cache = cache_args(*cache);
+    a.page_table = page_table, a.table_pages = table_pages, a.lengths = lengths, a.requests = n_requests;
+    a.row_start = row_start, a.max_rows = max_rows, a.tail_mask = tail_mask;
+    a.window = (int)window, a.sinks = (int)sinks, a.positions = indexes(positions, pos_type);
+    const int64_t held = (int64_t)table_pages * cache->page_size;
+    a.most = (int)(max_length < held ? max_length : held);
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.out = out, a.out_stride = out_stride, a.lse = out_lse;
+    a.whole = split.whole, a.places = split.places, a.row_blocks = split.row_blocks, a.row_tiles = split.row_tiles;
+    a.G_magic = (unsigned)(((uint64_t)1 << 32) / a.G) + 1u;
+    a.by_place = n_requests > split.places;
+    a.part_o = static_cast<float *>(ws);
+    a.part_ms = reinterpret_cast<float2 *>(a.part_o + split.entries * cache->head_dim);
+    a.part_at = reinterpret_cast<int4 *>(a.part_ms + split.entries);
+    return vt::status_of_hip(vt::launch_attend(a, f32, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -229,36 +277,20 @@ int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int
                        int32_t table_pages, const int32_t *lengths, int32_t n_requests, const int32_t *row_start, int32_t max_rows,
                        const uint64_t *tail_mask, int64_t max_length, float scale, void *out, int64_t out_stride, float *out_lse, void *ws,
                        size_t ws_bytes, void *stream) {
-    int s = cache_status(cache);
-    if (s != VT_OK) return s;
-    if (!element(type)) return VT_ERR_DTYPE;
-    const bool f32 = type == VT_F32;
-    const Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32);
-    if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
-    if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
-    if (n == 0 || n_requests == 0) return VT_OK;
-    if (page_table == nullptr || lengths == nullptr) return VT_ERR_NULL;
-    if ((s = heads_status(q, q_stride, q_heads, cache->head_dim)) != VT_OK) return s;
-    if ((s = heads_status(out, out_stride, q_heads, cache->head_dim)) != VT_OK) return s;
-    if (!aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(row_start, 4) || !aligned(tail_mask, 8)) return VT_ERR_ALIGN;
-    if (split.bytes > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < split.bytes)) return VT_ERR_WORKSPACE;
-    if (!aligned(out_lse, 4)) return VT_ERR_ALIGN;
-    vt::AttendArgs a{};
-    a.q = q, a.q_stride = q_stride, a.n = (int)n, a.hq = q_heads, a.G = q_heads / cache->heads;
-    a.cache = cache_args(*cache);
-    a.page_table = page_table, a.table_pages = table_pages, a.lengths = lengths, a.requests = n_requests;
-    a.row_start = row_start, a.max_rows = max_rows, a.tail_mask = tail_mask;
-    const int64_t held = (int64_t)table_pages * cache->page_size;
-    a.most = (int)(max_length < held ? max_length : held);
-    a.scale_log2 = scale * 1.4426950408889634f;
-    a.out = out, a.out_stride = out_stride, a.lse = out_lse;
-    a.whole = split.whole, a.places = split.places, a.row_blocks = split.row_blocks, a.row_tiles = split.row_tiles;
-    a.G_magic = (unsigned)(((uint64_t)1 << 32) / a.G) + 1u;
-    a.by_place = n_requests > split.places;
-    a.part_o = static_cast<float *>(ws);
-    a.part_ms = reinterpret_cast<float2 *>(a.part_o + split.entries * cache->head_dim);
-    a.part_at = reinterpret_cast<int4 *>(a.part_ms + split.entries);
-    return vt::status_of_hip(vt::launch_attend(a, f32, static_cast<hipStream_t>(stream)));
+    return attention(q, q_stride, type, n, q_heads, cache, page_table, table_pages, lengths, n_requests, row_start, max_rows, tail_mask, 0, 0, nullptr,
+                     VT_I32, max_length, scale, out, out_stride, out_lse, ws, ws_bytes, stream);
+}
+
+int vt_paged_attention_window(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache,
+                              const int32_t *page_table, int32_t table_pages, const int32_t *lengths, int32_t n_requests, const int32_t *row_start,
+                              int32_t max_rows, const uint64_t *tail_mask, const void *positions, int pos_type, int64_t window, int64_t sinks,
+                              int64_t max_length, float scale, void *out, int64_t out_stride, float *out_lse, void *ws, size_t ws_bytes,
+                              void *stream) {
+    if (positions != nullptr && !index_type(pos_type)) return VT_ERR_DTYPE;
+    if (window < 1 || window > kMaxLength || sinks < 0 || sinks > kMaxLength || (positions != nullptr && tail_mask == nullptr)) return VT_ERR_SHAPE;
+    if (!index_aligned(positions, pos_type)) return VT_ERR_ALIGN;
+    return attention(q, q_stride, type, n, q_heads, cache, page_table, table_pages, lengths, n_requests, row_start, max_rows, tail_mask, window, sinks,
+                     positions, pos_type, max_length, scale, out, out_stride, out_lse, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

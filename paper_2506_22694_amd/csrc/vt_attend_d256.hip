@@ -4,7 +4,7 @@
 namespace vt {
 
 hipError_t launch_attend_d256(const AttendArgs &a, int, bool f32, hipStream_t st) {
-    return f32 ? run_attend<256, 1, true>(a, st) : run_attend<256, 1, false>(a, st);
+    return f32 ? run_attend<256, 1, true, false>(a, st) : run_attend<256, 1, false, false>(a, st);
 }
 
 }  // namespace vt

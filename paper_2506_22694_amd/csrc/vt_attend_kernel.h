@@ -36,10 +36,26 @@ typedef __attribute__((ext_vector_type(4))) float f32x4a;
 __device__ __forceinline__ f32x4a mfma(u32x4 a, u32x4 b, f32x4a c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-// bf16 pairs of two codes: the lower or upper two of a register
+// What a cache holds: bf16, or codes of 8 or 4 bits
+constexpr int kHeld16 = 0, kHeld8 = 1, kHeld4 = 2;
+
+// bf16 pairs of two codes of 8 bits: the lower or upper two of a register
 template <bool HIGH>
 __device__ __forceinline__ unsigned two_codes(unsigned u) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH));
+}
+// ... of the eight codes of 4 bits of a register, times a power of two: the scale's bits 30 to 23 are its exponent + 127, all other bits count for nothing
+__device__ __forceinline__ void eight_codes(unsigned u, unsigned scale, unsigned (&f)[4]) {
+    const float s = __uint_as_float(scale);
+    f[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 0));
+    f[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 1));
+    f[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 2));
+    f[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 3));
+}
+__device__ __forceinline__ void four_codes(unsigned u, unsigned scale, unsigned (&f)[2]) {
+    const float s = __uint_as_float(scale);
+    f[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 0));
+    f[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, s, 1));
 }
 // Maximum and sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48, which hold the same row
 __device__ __forceinline__ float row_max(float v) {
@@ -90,6 +106,11 @@ __device__ __forceinline__ void store_values(const AttendArgs &a, int64_t at, co
 // y / G for y < 2048, G <= 1024
 __device__ __forceinline__ int by_group(const AttendArgs &a, int y) { return a.G == 1 ? y : (int)__umulhi((unsigned)y, a.G_magic); }
 
+// Row i of a request's rows, `row` of all
+__device__ __forceinline__ int position_of(const AttendArgs &a, int64_t row, int tokens, int rows, int i) {
+    return a.positions.p != nullptr ? given_position(tokens, index_at(a.positions, row)) : last_position(tokens, rows, i);
+}
+
 // Sums over the lanes up to and including each
 __device__ __forceinline__ int wave_scan(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr:1, 2, 4, 8
@@ -101,13 +122,16 @@ __device__ __forceinline__ int wave_scan(int v) {
     return v;
 }
 // A request: its cached tokens that are looked at, its new rows and where they begin
+// With a window, tokens are counted without the `gap` of those between the sinks and the window, which no row sees.
 struct Request {
-    int tokens, rows, first;
+    int tokens, rows, first, gap;
 };
+template <bool WINDOW>
 __device__ __forceinline__ Request request_of(const AttendArgs &a, int b) {
     int first;
-    const int rows = rows_of(a.row_start, b, a.n, a.max_rows, first);
-    return {tokens_of(a.lengths[b], a.most), rows, first};
+    const int rows = rows_of(a.row_start, b, a.n, a.max_rows, first), tokens = tokens_of(a.lengths[b], a.most);
+    const int gap = WINDOW ? window_gap(tokens, a.positions.p != nullptr ? kTail : rows, a.window, a.sinks) : 0;
+    return {tokens - gap, rows, first, gap};
 }
 __device__ __forceinline__ int request_steps(const Request &r) { return steps_of(r.tokens, r.rows, kAttendStep); }
 
@@ -117,9 +141,10 @@ struct Share {
     Request r;
     int b, at, left, per;
 };
+template <bool WINDOW>
 __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     const int lane = lane_id();
-    auto request = [&](int i) { return i < a.requests ? request_of(a, i) : Request{0, 0, 0}; };
+    auto request = [&](int i) { return i < a.requests ? request_of<WINDOW>(a, i) : Request{0, 0, 0, 0}; };
     Request r = request(lane);
     const int mine = request_steps(r);
     int sum = mine;
@@ -150,7 +175,8 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
     const int at = __builtin_ctzll(__ballot(before + upto > start));
     s.b = base + at;
     s.at = start - before - (at == 0 ? 0 : __builtin_amdgcn_readlane(upto, at - 1));
-    s.r = {__builtin_amdgcn_readlane(r.tokens, at), __builtin_amdgcn_readlane(r.rows, at), __builtin_amdgcn_readlane(r.first, at)};
+    s.r = {__builtin_amdgcn_readlane(r.tokens, at), __builtin_amdgcn_readlane(r.rows, at), __builtin_amdgcn_readlane(r.first, at),
+           WINDOW ? __builtin_amdgcn_readlane(r.gap, at) : 0};
     return s;
 }
 
@@ -158,18 +184,20 @@ __device__ __forceinline__ Share share_of(const AttendArgs &a, int place) {
 // 16 bytes of it, and read 8 of those, the tail mask, in the tiles that it applies to).  Two at least, so that there are 256 vector
 // registers and no accumulation registers: copies out of those have come ahead of the matrix instructions' results here (a branch right
 // behind the last product: clang 20 leaves out the wait states on its way), which the build checks there are none of.
-template <int DP, bool FP8, int NT, bool F32Q>
+template <int DP, int HELD, int NT, bool F32Q>
 constexpr int attend_occupancy() {
     if (DP == 64) return NT == 1 ? 4 : NT == 2 ? 3 : 2;
     return 2;
 }
 
-template <int DP, bool FP8, int NT, bool F32Q>
-__global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F32Q>())) void attend_kernel(AttendArgs a) {
+template <int DP, int HELD, int NT, bool F32Q, bool WINDOW>
+__global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, F32Q>())) void attend_kernel(AttendArgs a) {
     constexpr int W = kAttendWaves, E = DP / 16, KS = DP / 32, TERMS = F32Q ? 3 : 1;      // (of q)
-    constexpr int KL = FP8 ? DP / 64 : DP / 32;       // 16-byte loads of a token's row of K in a lane
-    constexpr int VR = FP8 ? DP / 64 : DP / 32;       // registers of a token's E values of V
-    constexpr int SZ = FP8 ? 1 : 2;
+    constexpr bool FP8 = HELD == kHeld8, FP4 = HELD == kHeld4;
+    constexpr int KL = FP4 ? (DP + 127) / 128 : FP8 ? DP / 64 : DP / 32;      // loads of a token's row of K in a lane, of 16 bytes (FP4, DP = 64: of 8)
+    constexpr int VR = FP4 ? (DP + 127) / 128 : FP8 ? DP / 64 : DP / 32;      // registers of a token's E values of V
+    constexpr int BITS = FP4 ? 4 : FP8 ? 8 : 16;
+    auto bytes = [](int values) { return values * BITS / 8; };
     constexpr int PITCH = DP + 4;
     // Rows of 256 values have no registers for a tile's keys and values at a time: values are asked for when the keys are used up, and
     // another wave's loads fill the time.
@@ -191,10 +219,10 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
     if (a.whole) {
         share.b = place;
         share.at = share.per = 0;
-        share.r = request_of(a, place);
+        share.r = request_of<WINDOW>(a, place);
         share.left = request_steps(share.r);
     } else {
-        share = share_of(a, place);
+        share = share_of<WINDOW>(a, place);
         if (share.left == 0 && a.by_place && blockIdx.x == 0 && threadIdx.x == 0) a.part_at[place] = make_int4(place, 1, 0, 0);
     }
 
@@ -204,7 +232,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         int thread = threadIdx.x;
         asm volatile("" : "+v"(thread));
         const int lane = thread & 63, m = lane & 15, g = lane >> 4;
-        const int b = share.b, at_step = share.at, len = share.r.tokens, nrows = share.r.rows;
+        const int b = share.b, at_step = share.at, len = share.r.tokens, nrows = share.r.rows, gap = share.r.gap;
         const int64_t first = share.r.first;
         const int32_t *pages = a.page_table + (int64_t)b * a.table_pages;
         int window = 0, ids = pages[min(lane, a.table_pages - 1)];
@@ -213,7 +241,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         share.left -= take;
         if (share.left > 0) {
             if (share.b + 1 >= a.requests) share.left = 0;      // (lengths that are written to meanwhile)
-            else share.r = request_of(a, ++share.b);
+            else share.r = request_of<WINDOW>(a, ++share.b);
             share.at = 0;
         }
         // For the join: where the parts of each request are, or of the one request that a place may begin and not end.
@@ -234,14 +262,20 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         // values of d that the lane's K has
         u32x4 q[NT][KS * (F32Q ? 2 : 1)];
         uint64_t tail[NT];
+        int from[NT], upto[NT];      // WINDOW: tokens that the row sees beside the sinks
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int x = 16 * nt + m, y = x0_head + min(x, RG - 1), up = by_group(a, y);
             const int64_t row = first + x0_row + up, at = row * a.q_stride + (h * a.G + y - up * a.G) * D;
             tail[nt] = a.tail_mask != nullptr ? a.tail_mask[row] : 0;
+            if constexpr (WINDOW) {
+                const int position = position_of(a, row, len + gap, nrows, x0_row + up);
+                from[nt] = position - a.window + 1;
+                upto[nt] = a.tail_mask != nullptr ? INT32_MAX : position;
+            }
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const int d = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+                const int d = FP4 ? DP / 4 * g + 8 * s : FP8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
                 const bool there = x < RG && d < D;
                 const int64_t from = at + (d < D ? d : 0);
 #pragma unroll
@@ -259,16 +293,19 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 
         // Page numbers of 64 pages, one in each lane.  (The empty asm has the wait for them where they are loaded: at the join of the branch it
         // would be for all loads under way.)
-        const int last_page = max(len - 1, 0) >> shift;
-        if (t0 >> shift >= 64) {
-            window = t0 >> shift;
+        const int last_page = max(len + gap - 1, 0) >> shift;
+        // (the token that is counted as the t-th)
+        const int sinks16 = WINDOW ? round16(a.sinks) : 0;
+        auto real = [&](int t) { return WINDOW && t >= sinks16 ? t + gap : t; };
+        if (real(t0) >> shift >= 64) {
+            window = real(t0) >> shift;
             ids = pages[min(window + lane, last_page)];
         }
         asm volatile("" : "+v"(ids));
         // First row of 16 tokens (of one page: pages are multiples of 16) in the cache, or -1 where there is nothing to read.
-        auto rows16 = [&](int token) -> int64_t {
-            if (token >= t1) return -1;
-            const int p = token >> shift;
+        auto rows16 = [&](int t) -> int64_t {
+            if (t >= t1) return -1;
+            const int token = real(t), p = token >> shift;
             if (p >= window + 64) {
                 window = p;
                 ids = pages[min(p + lane, last_page)];
@@ -285,34 +322,57 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         int k_at[KL];
 #pragma unroll
         for (int s = 0; s < KL; ++s) {
-            const int d = FP8 ? 64 * s + 16 * g : 32 * s + 8 * g;
-            k_at[s] = d < D ? (m * D + d) * SZ : kBeyond;
+            const int d = FP4 ? DP / 4 * g + 32 * s : FP8 ? 64 * s + 16 * g : 32 * s + 8 * g;
+            k_at[s] = d < D ? bytes(m * D + d) : kBeyond;
         }
-        const int v_at = E * m < D ? (4 * g * D + E * m) * SZ : kBeyond;
+        const int v_at = E * m < D ? bytes(4 * g * D + E * m) : kBeyond;
         auto buffer = [&](const void *base, int64_t row, int row_bytes) {
             return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(static_cast<const char *>(base) + (row < 0 ? 0 : row) * row_bytes), 0,
                                                      row < 0 ? 0 : 16 * row_bytes, 0x00027000);
         };
+        // 4 bits: scales of the 16 rows' groups, group j's `1 << shift` bytes after those of group j - 1
+        auto scales_of_four = [&](const uint8_t *base, int64_t row) {
+            const int groups = D / kScaleGroup;
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base + (row < 0 ? 0 : scale_of_row(row, groups, 0, shift))), 0,
+                                                     row < 0 ? 0 : ((groups - 1) << shift) + 16, 0x00027000);
+        };
+        const int v_scale_at = FP4 ? (E * m < D ? ((E * m / kScaleGroup) << shift) + 4 * g : kBeyond) : 4 * g;
 
         u32x4 k[2][KL];
-        unsigned v[8][VR], k_scale[2] = {}, v_scale[2] = {};
+        unsigned v[8][VR], k_scale[2][FP4 ? KL : 1] = {}, v_scale[2] = {};
         auto load_k = [&](const int64_t (&row)[2]) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const auto r = buffer(a.cache.k, row[t], D * SZ);
+                const auto r = buffer(a.cache.k, row[t], bytes(D));
 #pragma unroll
-                for (int s = 0; s < KL; ++s) k[t][s] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at[s], 0, kNt);
-                if constexpr (FP8) k_scale[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.cache.k_scale, row[t], 1), 4 * g, 0, 0);
+                for (int s = 0; s < KL; ++s) {
+                    if constexpr (FP4 && DP == 64) {
+                        const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(r, k_at[s], 0, kNt);
+                        k[t][s].x = u.x, k[t][s].y = u.y;
+                    } else {
+                        k[t][s] = __builtin_amdgcn_raw_buffer_load_b128(r, k_at[s], 0, kNt);
+                    }
+                }
+                if constexpr (FP8) k_scale[t][0] = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.cache.k_scale, row[t], 1), 4 * g, 0, 0);
+                if constexpr (FP4) {
+#pragma unroll
+                    for (int s = 0; s < KL; ++s) {
+                        const int d = DP / 4 * g + 32 * s;
+                        k_scale[t][s] = __builtin_amdgcn_raw_buffer_load_b8(scales_of_four(a.cache.k_scale, row[t]), d < D ? ((d / kScaleGroup) << shift) + m : kBeyond, 0, 0);
+                    }
+                }
             }
         };
         auto load_v = [&](const int64_t (&row)[2]) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const auto buf = buffer(a.cache.v, row[t], D * SZ);
+                const auto buf = buffer(a.cache.v, row[t], bytes(D));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = v_at + i * D * SZ, j = 4 * t + i;
-                    if constexpr (VR == 1) {
+                    const int at = v_at + i * bytes(D), j = 4 * t + i;
+                    if constexpr (FP4 && DP == 64) {
+                        v[j][0] = __builtin_amdgcn_raw_buffer_load_b16(buf, at, 0, kNt);
+                    } else if constexpr (VR == 1) {
                         v[j][0] = __builtin_amdgcn_raw_buffer_load_b32(buf, at, 0, kNt);
                     } else if constexpr (VR == 2) {
                         const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(buf, at, 0, kNt);
@@ -325,7 +385,8 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                         }
                     }
                 }
-                if constexpr (FP8) v_scale[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.cache.v_scale, row[t], 1), 4 * g, 0, 0);
+                if constexpr (FP8) v_scale[t] = __builtin_amdgcn_raw_buffer_load_b32(buffer(a.cache.v_scale, row[t], 1), v_scale_at, 0, 0);
+                if constexpr (FP4) v_scale[t] = __builtin_amdgcn_raw_buffer_load_b32(scales_of_four(a.cache.v_scale, row[t]), v_scale_at, 0, 0);
             }
         };
 
@@ -339,8 +400,29 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
         }
 
         // Registers of V as operands of the product over its values 2 r, 2 r + 1 (16 bits) or 4 r .. 4 r + 3 (codes)
-        constexpr int VF = FP8 ? 4 : 2;
+        // (4 bits: 8 r .. 8 r + 7, or 0 .. 3; their scales are in them, as `v_scale` differs from one 32 values to the next)
+        constexpr int VF = FP4 ? (DP == 64 ? 4 : 8) : FP8 ? 4 : 2;
         auto operands = [&](int r, u32x4 (&f)[VF]) {
+            if constexpr (FP4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    unsigned one[VF / 2], two[VF / 2];
+                    auto scale_of = [&](int i) { return i % 4 == 0 ? v_scale[i / 4] << 23 : i % 4 == 1 ? v_scale[i / 4] << 15 : i % 4 == 2 ? v_scale[i / 4] << 7 : v_scale[i / 4] >> 1; };
+                    if constexpr (VF == 8) {
+                        eight_codes(v[2 * j][r], scale_of(2 * j), one);
+                        eight_codes(v[2 * j + 1][r], scale_of(2 * j + 1), two);
+                    } else {
+                        four_codes(v[2 * j][r], scale_of(2 * j), one);
+                        four_codes(v[2 * j + 1][r], scale_of(2 * j + 1), two);
+                    }
+#pragma unroll
+                    for (int i = 0; i < VF; i += 2) {
+                        f[i][j] = __builtin_amdgcn_perm(two[i / 2], one[i / 2], 0x05040100);
+                        f[i + 1][j] = __builtin_amdgcn_perm(two[i / 2], one[i / 2], 0x07060302);
+                    }
+                }
+                return;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (!FP8) {
@@ -390,6 +472,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                         }
                     }
                 }
+                if constexpr (FP4) continue;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     constexpr unsigned part = FP8 ? 0xFFu : 0xFFFFu, step = FP8 ? 8 : 16, odd = FP8 ? 0x7Fu : 0x7F80u;
@@ -400,6 +483,21 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                         clean |= ((u & odd) == odd ? 0u : u) << at;
                     }
                     v[j][r] = clean;
+                }
+            }
+            if constexpr (FP4) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    // the first magnitude that is infinite: 4 * 2^126, 2 * 2^127; of 255 all are NaN
+                    const unsigned scale = (v_scale[j / 4] >> 8 * (j % 4)) & 0xFF, first = scale < 253 ? 8 : scale == 253 ? 6 : scale == 254 ? 4 : 0;
+#pragma unroll
+                    for (int r = 0; r < VR; ++r) {
+                        unsigned clean = 0;
+#pragma unroll
+                        for (int at = 0; at < 32; at += 4) clean |= ((v[j][r] >> at) & 7) < first ? v[j][r] & (15u << at) : 0u;
+                        v[j][r] = clean;
+                    }
+                    if (scale == 255) v_scale[j / 4] &= ~(0xFFu << 8 * (j % 4));
                 }
             }
         };
@@ -432,7 +530,11 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         u32x4 f;
-                        if constexpr (FP8) {
+                        if constexpr (FP4) {
+                            unsigned pairs[4];
+                            eight_codes(k[t][c / 4][c % 4], k_scale[t][c / 4] << 23, pairs);
+                            f = u32x4{pairs[0], pairs[1], pairs[2], pairs[3]};
+                        } else if constexpr (FP8) {
                             const unsigned u0 = k[t][c / 2][2 * (c % 2)], u1 = k[t][c / 2][2 * (c % 2) + 1];
                             f = u32x4{two_codes<false>(u0), two_codes<true>(u0), two_codes<false>(u1), two_codes<true>(u1)};
                         } else {
@@ -450,7 +552,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                 for (int t = 0; t < 2; ++t) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        factor[t][i] = FP8 ? scaled(a.scale_log2, (k_scale[t] >> 8 * i) & 0xFF) : a.scale_log2;
+                        factor[t][i] = FP8 ? scaled(a.scale_log2, (k_scale[t][0] >> 8 * i) & 0xFF) : a.scale_log2;
                 }
 
                 // the next tile's keys are asked for once this one's are used up, its values likewise below
@@ -460,7 +562,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                 else load_v(row);
 
                 const bool ends = token + kAttendTile > t1 || row[0] < 0 || row[1] < 0;
-                const bool masked = a.tail_mask != nullptr && token + kAttendTile > len - 64;
+                const int tokens[2] = {real(token), real(token + 16)};      // first ones of the two 16
+                const bool tail_masked = a.tail_mask != nullptr && tokens[1] + 16 > len + gap - kTail;
+                bool masked = tail_masked;
+                if constexpr (WINDOW) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) masked |= __any((tokens[t] < from[nt] && tokens[t] + 15 >= a.sinks) || tokens[t] + 15 > upto[nt]) != 0;
+                    }
+                }
                 // bit i: whether there is a token 16 t + 4 g + i
                 unsigned there[2] = {15, 15};
                 if (ends) {
@@ -482,10 +593,17 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             unsigned seen = there[t];
-                            if (masked) {
-                                const int bit = token + 16 * t + 4 * g - (len - 64);      // of the first of the four; bits before the first: seen
+                            if (tail_masked) {
+                                const int bit = tokens[t] + 4 * g - (len + gap - kTail);      // of the first of the four; bits before the first: seen
                                 const unsigned bits = (unsigned)(tail[nt] >> min(max(bit, 0), 63)), before = min(max(-bit, 0), 4);
                                 seen &= (bit < 64 ? bits << before : 0u) | ((1u << before) - 1u);
+                            }
+                            if constexpr (WINDOW) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const int at = tokens[t] + 4 * g + i;
+                                    if ((at < from[nt] && at >= a.sinks) || at > upto[nt]) seen &= ~(1u << i);
+                                }
                             }
 #pragma unroll
                             for (int i = 0; i < 4; ++i) z[t][i] = (seen >> i) & 1 ? z[t][i] : kNone;
@@ -530,6 +648,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     for (int j = 0; j < 8; ++j) {
 #pragma unroll
                         for (int r = 0; r < VR; ++r) v[j][r] = (there[j / 4] >> j % 4) & 1 ? v[j][r] : 0u;
+                        if constexpr (FP4) v_scale[j / 4] &= (there[j / 4] >> j % 4) & 1 ? ~0u : ~(0xFFu << 8 * (j % 4));
                     }
                 }
                 bool hard = false;
@@ -539,9 +658,14 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
                     for (int j = 0; j < 8; ++j) {
 #pragma unroll
                         for (int r = 0; r < VR; ++r) {
-                            if constexpr (FP8) odd |= ((v[j][r] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+                            if constexpr (FP4) continue;
+                            else if constexpr (FP8) odd |= ((v[j][r] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
                             else odd |= ((v[j][r] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
                         }
+                    }
+                    if constexpr (FP4) {      // a scale of 253 or more
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) odd |= ((v_scale[t] & 0x7F7F7F7Fu) + 0x03030303u) & v_scale[t] & 0x80808080u;
                     }
                     hard = __any(odd != 0);
                 }
@@ -637,15 +761,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, FP8, NT, F
     }
 }
 
-template <int DP, bool FP8, int NT, bool F32Q>
+template <int DP, int HELD, int NT, bool F32Q, bool WINDOW>
 hipError_t run_attend(const AttendArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.cache.heads * a.row_blocks), (unsigned)a.places);
-    attend_kernel<DP, FP8, NT, F32Q><<<grid, 64 * kAttendWaves, 0, st>>>(a);
+    attend_kernel<DP, HELD, NT, F32Q, WINDOW><<<grid, 64 * kAttendWaves, 0, st>>>(a);
     return hipGetLastError();
 }
-template <int DP, int NT, bool F32Q>
+template <int DP, int NT, bool F32Q, bool WINDOW>
 hipError_t run_attend(const AttendArgs &a, hipStream_t st) {
-    return a.cache.k_scale != nullptr ? run_attend<DP, true, NT, F32Q>(a, st) : run_attend<DP, false, NT, F32Q>(a, st);
+    if (a.cache.four) return run_attend<DP, kHeld4, NT, F32Q, WINDOW>(a, st);
+    return a.cache.k_scale != nullptr ? run_attend<DP, kHeld8, NT, F32Q, WINDOW>(a, st) : run_attend<DP, kHeld16, NT, F32Q, WINDOW>(a, st);
 }
 
 }  // namespace vt

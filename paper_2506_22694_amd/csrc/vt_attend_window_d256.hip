@@ -1,0 +1,10 @@
+// Attention over the cache with a window and sinks, heads of up to 256 values.
+#include "vt_attend_kernel.h"
+
+namespace vt {
+
+hipError_t launch_attend_window_d256(const AttendArgs &a, int, bool f32, hipStream_t st) {
+    return f32 ? run_attend<256, 1, true, true>(a, st) : run_attend<256, 1, false, true>(a, st);
+}
+
+}  // namespace vt

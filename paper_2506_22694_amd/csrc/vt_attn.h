@@ -10,6 +10,7 @@ struct CacheArgs {
     uint8_t *k_scale, *v_scale;      // null: held in bf16
     int64_t pages;
     int heads, page_shift, D;
+    int four;                        // codes of 4 bits, two to a byte; scales of 32 values (else of a row)
 };
 
 // One row of positions or slots, of either index type.
@@ -63,6 +64,8 @@ struct AttendArgs {
     const int32_t *row_start;
     int max_rows;
     const uint64_t *tail_mask;
+    int window, sinks;       // 0: no window
+    IndexArgs positions;     // of rows with a tail mask and a window; null: a request's rows are its last tokens
     int most;          // tokens of a request that are looked at
     float scale_log2;
     void *out;
@@ -89,6 +92,10 @@ constexpr int kAttendStep = kAttendWaves * kAttendTile;          // ... and a wo
 hipError_t launch_attend_d64(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
 hipError_t launch_attend_d128(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
 hipError_t launch_attend_d256(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
+// csrc/vt_attend_window_d*.hip
+hipError_t launch_attend_window_d64(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
+hipError_t launch_attend_window_d128(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
+hipError_t launch_attend_window_d256(const AttendArgs &a, int tiles, bool f32, hipStream_t st);
 
 // The status of a HIP call's result, remembered for vt_last_device_error (csrc/vt_api.hip)
 int status_of_hip(hipError_t e);

@@ -220,6 +220,7 @@ decltype(&vt_qk_norm_rope_backward_ws_bytes) g_norm_backward_ws = nullptr;
 decltype(&vt_qkv_to_cache) g_to_cache = nullptr;
 decltype(&vt_kv_cache_read) g_read = nullptr;
 decltype(&vt_paged_attention) g_attend = nullptr;
+decltype(&vt_paged_attention_window) g_attend_window = nullptr;
 
 bool given(PyObject *o) { return o != Py_None; }
 // A gradient is asked for of the tensor, or it has a tangent: autograd's business, or a refusal
@@ -432,10 +433,11 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     });
 }
 
-// attend(q, cache address, page_table, lengths, row_start, max_rows, tail_mask, max_length, scale, workspace, out, return_lse, out_lse)
+// attend(q, cache address, page_table, lengths, row_start, max_rows, tail_mask, max_length, scale, workspace, out, return_lse, out_lse, window, sinks,
+// positions)
 PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     return result_of([&]() -> PyObject * {
-        if (n_args != 13 || g_attend == nullptr) throw NotPlain();
+        if (n_args != 16 || g_attend == nullptr || g_attend_window == nullptr) throw NotPlain();
         const Heads q = heads_of(a[0]);
         const vt_kv_cache *const cache = cache_of(a[1]);
         const at::Tensor &table = operand(a[2]), &lengths = operand(a[3]), &ws = operand(a[9]);
@@ -460,6 +462,15 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         }
         const int64_t most = given(a[7]) ? int32(a[7]) : (int64_t)pages * cache->page_size;
         const float scale = given(a[8]) ? (float)number(a[8]) : (float)std::pow((double)q.D, -0.5);
+        const bool windowed = given(a[13]);
+        const int64_t window = windowed ? int32(a[13]) : 0, sinks = int32(a[14]);
+        Index positions;
+        if (given(a[15])) {
+            if (mask == nullptr) throw NotPlain();
+            positions = Index(a[15]);
+            if (positions.n != q.n) throw NotPlain();
+        }
+        if (!windowed && (sinks != 0 || positions.p != nullptr)) throw NotPlain();
         const Heads out = result(a[10], q);
         const bool with_lse = truth(a[11]);
         at::Tensor lse;
@@ -475,20 +486,24 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         void *const wsp = ws.data_ptr(), *const stream = stream_of(q.t);
         const size_t ws_bytes = (size_t)ws.numel();
         const int status = unlocked([&] {
-            return g_attend(q.p, q.stride, type, q.n, q.heads, cache, pt, pages, len, requests, start, max_rows, mask, most, scale, out.p, out.stride, pl,
-                            wsp, ws_bytes, stream);
+            if (!windowed)
+                return g_attend(q.p, q.stride, type, q.n, q.heads, cache, pt, pages, len, requests, start, max_rows, mask, most, scale, out.p, out.stride,
+                                pl, wsp, ws_bytes, stream);
+            return g_attend_window(q.p, q.stride, type, q.n, q.heads, cache, pt, pages, len, requests, start, max_rows, mask, positions.p,
+                                   positions.type, window, sinks, most, scale, out.p, out.stride, pl, wsp, ws_bytes, stream);
         });
         if (status != VT_OK) return PyLong_FromLong(status);
         return with_lse ? tuple_of(wrap(out.t), wrap(lse)) : wrap(out.t);
     });
 }
 
-// connect(raw_stream, step, step_static, level, rerank, count, norm, norm_backward, its workspace's size, to_cache, cache_read, attend):
+// connect(raw_stream, step, step_static, level, rerank, count, norm, norm_backward, its workspace's size, to_cache, cache_read, attend,
+// attend_window):
 // torch's stream query and the addresses of the library's functions
 PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
-    constexpr int kFunctions = 11;
+    constexpr int kFunctions = 12;
     if (n_args != 1 + kFunctions) {
-        PyErr_SetString(PyExc_TypeError, "connect takes torch's stream query and eleven addresses");
+        PyErr_SetString(PyExc_TypeError, "connect takes torch's stream query and twelve addresses");
         return nullptr;
     }
     void *p[kFunctions];
@@ -510,6 +525,7 @@ PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     g_to_cache = reinterpret_cast<decltype(g_to_cache)>(p[8]);
     g_read = reinterpret_cast<decltype(g_read)>(p[9]);
     g_attend = reinterpret_cast<decltype(g_attend)>(p[10]);
+    g_attend_window = reinterpret_cast<decltype(g_attend_window)>(p[11]);
     Py_RETURN_NONE;
 }
 

@@ -6,6 +6,8 @@
 //
 // Bound by the bytes read and written: 4096 rows of 40 heads of 128 values in bf16 (84 MB) 16.5 us, 16384 rows 68 us, 4.9 TB/s, a copy's rate
 // of as much; gradients of 8192 rows (252 MB) 51 us and 4.6 for the weights' sums; 65537 rows of 8 heads read back from 8 bits (404 MB) 76 us.
+#include <type_traits>
+
 #include "vt_values.h"
 
 namespace vt {
@@ -78,14 +80,14 @@ __device__ __forceinline__ Angle angle_of(const NormArgs &a, const Lane &l, int6
     return t;
 }
 // x turned by +angle, or by -angle (SIGN = -1): the transpose, for gradients
-template <int SIGN>
-__device__ __forceinline__ void turn(float *x, const Angle &t, bool neighbours) {
-    float y[8];
+template <int SIGN, typename V>
+__device__ __forceinline__ void turn(V *x, const Angle &t, bool neighbours) {
+    V y[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float s = SIGN < 0 ? -t.s[j] : t.s[j];
-        const float a = neighbours ? x[2 * j] : x[j], b = neighbours ? x[2 * j + 1] : x[4 + j];
-        const float ra = a * t.c[j] - b * s, rb = b * t.c[j] + a * s;
+        const V s = SIGN < 0 ? -t.s[j] : t.s[j], c = t.c[j];
+        const V a = neighbours ? x[2 * j] : x[j], b = neighbours ? x[2 * j + 1] : x[4 + j];
+        const V ra = a * c - b * s, rb = b * c + a * s;
         y[j] = ra, y[4 + j] = rb;
     }
 #pragma unroll
@@ -122,11 +124,41 @@ __device__ __forceinline__ void to_cache(const CacheArgs &c, bool is_v, int64_t 
     if (l.pair == 0) (is_v ? c.v_scale : c.k_scale)[cell] = (uint8_t)e;
 }
 
+// The same in 4 bits.  The lanes exchange their values so that each has eight side by side: `row` is the group's D floats of LDS.
+__device__ __forceinline__ void to_cache_of_four(const CacheArgs &c, bool is_v, int64_t cell, const Lane &l, int lane, float *row, float *x) {
+    if (l.active) {
+        F32::store4(row + l.o0, x);
+        F32::store4(row + l.o1, x + 4);
+    }
+    // (a group is lanes of one wave, whose accesses to LDS are in order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (l.active) {
+        F32::load4(row + 8 * lane, x);
+        F32::load4(row + 8 * lane + 4, x + 4);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    unsigned m = 0;      // bits of the largest finite size of the four lanes' values, all ones for NaN among them
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const unsigned u = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+        m = max(m, u < 0x7F800000u ? u : u == 0x7F800000u ? 0u : ~0u);
+    }
+    m = max(m, dpp_mov<0xB1>(m));
+    m = max(m, dpp_mov<0x4E>(m));
+    if (!l.active || cell < 0) return;
+    const int e = m == ~0u ? 255 : scale_exponent_of_four(m);
+    *reinterpret_cast<unsigned *>(static_cast<uint8_t *>(is_v ? c.v : c.k) + cell * (c.D / 2) + 4 * lane) = m == ~0u ? 0u : pack_e2m1(x, e);
+    if (lane % 4 == 0) (is_v ? c.v_scale : c.k_scale)[scale_of_row(cell, c.D / kScaleGroup, lane / 4, c.page_shift)] = (uint8_t)e;
+}
+
 constexpr int kRowsAhead = 4;
 
-template <typename T, int GL, bool SEVERAL>
+// FOUR: into a cache of 4 bits.  Its keys are computed in 64 bits up to the rounding to a code: next to a border between two codes, where fp32's last bits
+// decide, the other one is up to half the value away.  (It costs nothing beside the bytes: MEASURED)
+template <typename T, int GL, bool SEVERAL, bool FOUR>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
     constexpr int GROUPS = kThreads / GL;
+    __shared__ __align__(16) float exchange[FOUR ? kThreads * 8 : 1];
     const int group = threadIdx.x / GL;
     const Lane l = lane_of(threadIdx.x % GL, a);
     const int heads = a.hq + a.hk + (a.v != nullptr ? a.hk : 0);
@@ -160,6 +192,26 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormArgs a) {
                 const int head = is_q ? r : is_v ? r - a.hq - a.hk : r - a.hq;
                 float x[8];
                 raw[u].open(x);
+                if constexpr (FOUR) {
+                    if (!is_q) {
+                        if (!is_v && (norm || a.table != nullptr)) {
+                            double z[8], ss = 0.0;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[j] = x[j], ss += z[j] * z[j];
+                            if (norm) {
+                                const double rms = 1.0 / sqrt(group_sum<GL>(ss) / a.D + a.eps);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) z[j] = z[j] * rms * wk[j];
+                            }
+                            if (l.turns) turn<1>(z, t, a.neighbours);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = round_to_odd(z[j]);
+                        }
+                        to_cache_of_four(a.cache, is_v, row_of_slot(slot, a.cache.pages, a.cache.heads, head, a.cache.page_shift), l, threadIdx.x % GL,
+                                         exchange + group * 8 * GL, x);
+                        continue;
+                    }
+                }
                 if (norm && !is_v) {
                     float ss = 0.0f;
 #pragma unroll
@@ -308,7 +360,11 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a) {
             const void *held = which ? a.cache.v : a.cache.k;
             float x[8] = {};
             if (cell >= 0) {
-                if (a.cache.k_scale == nullptr) {
+                if (a.cache.four) {
+                    const unsigned u = *reinterpret_cast<const unsigned *>(static_cast<const uint8_t *>(held) + cell * (a.cache.D / 2) + o / 2);
+                    const int64_t at = scale_of_row(cell, a.cache.D / kScaleGroup, o / kScaleGroup, a.cache.page_shift);
+                    open_e2m1(u, (which ? a.cache.v_scale : a.cache.k_scale)[at], x);
+                } else if (a.cache.k_scale == nullptr) {
                     const uint16_t *p = static_cast<const uint16_t *>(held) + cell * a.cache.D + o;
                     Bf16::load4(p, x);
                     Bf16::load4(p + 4, x + 4);
@@ -348,9 +404,14 @@ void run_forward(NormArgs a, hipStream_t st) {
     a.tokens_log2 = tokens_log2(a.n, a.hq + a.hk + (a.v != nullptr ? a.hk : 0), kThreads / GL);
     const dim3 grid(workgroups((a.n + ((int64_t)1 << a.tokens_log2) - 1) >> a.tokens_log2));
     auto launch = [&](auto one, auto several) { (a.tokens_log2 > 0 ? several : one)<<<grid, kThreads, 0, st>>>(a); };
-    if (GL == 8) launch(norm_rope_kernel<T, 8, false>, norm_rope_kernel<T, 8, true>);
-    else if (GL == 16) launch(norm_rope_kernel<T, 16, false>, norm_rope_kernel<T, 16, true>);
-    else launch(norm_rope_kernel<T, 32, false>, norm_rope_kernel<T, 32, true>);
+    auto held = [&](auto four) {
+        constexpr bool FOUR = decltype(four)::value;
+        if (GL == 8) launch(norm_rope_kernel<T, 8, false, FOUR>, norm_rope_kernel<T, 8, true, FOUR>);
+        else if (GL == 16) launch(norm_rope_kernel<T, 16, false, FOUR>, norm_rope_kernel<T, 16, true, FOUR>);
+        else launch(norm_rope_kernel<T, 32, false, FOUR>, norm_rope_kernel<T, 32, true, FOUR>);
+    };
+    if (a.to_cache && a.cache.four) held(std::true_type());
+    else held(std::false_type());
 }
 template <typename T>
 void run_backward(NormArgs a, hipStream_t st) {

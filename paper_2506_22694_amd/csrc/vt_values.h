@@ -61,6 +61,22 @@ template <int GL>
 __device__ __forceinline__ float group_sum(float v) {
     return group_reduce<GL>(v, OpAddF32{});
 }
+// ... of 64 bits
+template <int GL>
+__device__ __forceinline__ double group_sum(double v) {
+    auto part = [](double x, int high) { return (unsigned)(__double_as_longlong(x) >> (32 * high)); };
+    auto whole = [](unsigned lo, unsigned hi) { return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo)); };
+    v += whole(dpp_mov<0xB1>(part(v, 0)), dpp_mov<0xB1>(part(v, 1)));
+    v += whole(dpp_mov<0x4E>(part(v, 0)), dpp_mov<0x4E>(part(v, 1)));
+    v += whole(dpp_mov<0x141>(part(v, 0)), dpp_mov<0x141>(part(v, 1)));
+    if constexpr (GL >= 16) v += whole(dpp_mov<0x140>(part(v, 0)), dpp_mov<0x140>(part(v, 1)));
+    if constexpr (GL >= 32) {
+        const auto lo = __builtin_amdgcn_permlane16_swap(part(v, 0), part(v, 0), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(part(v, 1), part(v, 1), false, false);
+        v = whole(lo[0], hi[0]) + whole(lo[1], hi[1]);
+    }
+    return v;
+}
 template <int GL>
 __device__ __forceinline__ float group_max(float v) {
     return group_reduce<GL>(v, OpMaxF32{});
@@ -82,6 +98,34 @@ __device__ __forceinline__ unsigned pack_e4m3(const float *x, float inverse, flo
     }
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+}
+// A value of 64 bits as one of fp32 that any further rounding takes for the value itself: cut off, and odd where something was cut off, so that it lies
+// on the same side of every border and is on one only if the value is.
+__device__ __forceinline__ float round_to_odd(double x) {
+    const float f = (float)x;
+    unsigned u = __float_as_uint(f);
+    u -= fabs((double)f) > fabs(x) ? 1u : 0u;
+    return __uint_as_float((double)__uint_as_float(u) != x ? u | 1u : u);
+}
+// Eight values as 4-bit codes of the scale 2^(exponent - 127), the first one lowest.  (The conversion takes infinities and what is past 6 for 6.  With the
+// scale of the largest fp32 values 4 would be infinite: at most 3 there.)
+__device__ __forceinline__ unsigned pack_e2m1(const float *x, int exponent) {
+    const float most = exponent == 253 ? 3.0f * 0x1p126f : __FLT_MAX__, scale = __uint_as_float((unsigned)exponent << 23);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i], -most, most);
+    unsigned u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], scale, 0);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[2], y[3], scale, 1);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[4], y[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[6], y[7], scale, 3);
+}
+// The codes as values.  Scale 255 stands for NaN, which the conversion makes of it.
+__device__ __forceinline__ void open_e2m1(unsigned u, unsigned exponent, float *x) {
+    const float scale = __uint_as_float(exponent << 23);
+    typedef __attribute__((ext_vector_type(2))) float f32x2v;
+    const f32x2v a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, scale, 1);
+    const f32x2v c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(u, scale, 3);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
 }
 // x * 2^(exponent - 127) for every byte that a cache may hold: as a float's exponent bits, 0 would be no 2^-127 and 255 would make NaN of x = 0
 __device__ __forceinline__ float scaled(float x, unsigned exponent) { return __builtin_ldexpf(x, (int)exponent - 127); }
