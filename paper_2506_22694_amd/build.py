@@ -58,7 +58,7 @@ MIN_LDS_LOADS = {"vt_head_mfma_rows.hip": 1950}
 # The attention kernels may use no accumulation registers: the compiler's copies out of them have come ahead of the matrix instructions' results
 # (a copy three instructions behind the last product, on the far side of a branch: clang 20 leaves out the wait states on that way, and
 # scores came out wrong).  Cut to 256 vector registers they need none.
-NO_ACCUMULATION = ("vt_attend_d", "vt_attend_window_d")
+NO_ACCUMULATION = ("vt_attend_d", "vt_attend_window_d", "vt_prompt")
 
 # The sources with buffer loads, which are checked for scalar offsets that the descriptor's size may not cover.
 BUFFER_LOADS = ("vt_count.hip",)

@@ -80,6 +80,9 @@ constexpr int64_t kAttendWorkgroups = 512, kAttendWorkgroupsOfOne = 256;
 // workgroups: 13.2 and 11.2; 64 requests of up to 4000: 60.5 and 46.0).
 constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
+// Query rows of a kv head and request from which on a chunk goes through LDS, and workgroups from which on each has 128 of them and not 64.
+constexpr int64_t kPromptRows = 64, kPromptWorkgroups = 256;
+
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32) {
     Split s;
     if (n < 0 || n >= kMaxRows || q_heads < 1 || q_heads > VT_MAX_ATTENTION_HEADS || kv_heads < 1 || q_heads % kv_heads != 0 || D < 16 || D > VT_MAX_HEAD_DIM ||
@@ -130,7 +133,17 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
         // (what the workspace's size is asked with)
         if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32).ok) return VT_ERR_SHAPE;
     }
-    const Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32);
+    // rows of a chunk: tiles that many of them share
+    const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
+    const bool prompt = window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows;
+    Split split;
+    if (prompt) {
+        split.ok = true;
+        split.row_tiles = cache->head_dim > 128 || (chunk + 127) / 128 * cache->heads * n_requests < kPromptWorkgroups ? 1 : 2;
+        split.row_blocks = (int)((chunk + 64 * split.row_tiles - 1) / (64 * split.row_tiles));
+    } else {
+        split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32);
+    }
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
     if (n == 0 || n_requests == 0) return VT_OK;
@@ -156,6 +169,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     a.part_o = static_cast<float *>(ws);
     a.part_ms = reinterpret_cast<float2 *>(a.part_o + split.entries * cache->head_dim);
     a.part_at = reinterpret_cast<int4 *>(a.part_ms + split.entries);
+    if (prompt) return vt::status_of_hip(vt::launch_prompt(a, static_cast<hipStream_t>(stream)));
     return vt::status_of_hip(vt::launch_attend(a, f32, static_cast<hipStream_t>(stream)));
 }
 

@@ -83,6 +83,8 @@ struct AttendArgs {
 // 16-row tiles of queries that one workgroup takes
 int attend_row_tiles(int rows, int D, bool f32);
 hipError_t launch_attend(const AttendArgs &a, bool f32, hipStream_t st);
+// Rows that are a request's last tokens, with a window: row_blocks blocks of 64 row_tiles query rows (csrc/vt_prompt.hip)
+hipError_t launch_prompt(const AttendArgs &a, hipStream_t st);
 
 constexpr int kAttendWaves = 4;
 constexpr int kAttendTile = 32;                                   // cached tokens that a wave takes at a time

@@ -1,0 +1,344 @@
+// Attention of many rows of a request at a time -- a prompt's chunk -- over the cache with a sliding window and sinks, on the matrix cores.
+//
+// Bound by the products: a row of q meets every token of its window, and a workgroup's 64 NT query rows share what is read, so that the cache's
+// bytes are few beside them.  Tiles of TN tokens go through LDS, as bf16 whatever the cache holds, twice: one is computed on while the next one's
+// loads are under way.  Each of the four waves has 16 NT query rows (the heads that share a kv head, times new tokens) of its own:
+//
+//   scores^T [token, row] = K q^T      K's operand: a token's 16 bytes in a lane, from LDS; q stays in registers
+//   out^T [d, row] = V^T p^T           V's operand: four tokens of one column in a lane, by the transposing read of LDS; p's operand is what the
+//                                      first product leaves in a lane, so the running maxima and sums are a lane's own
+//
+// 16 bytes c of token t lie at place c ^ (t & 7) of the token's row in LDS: the eight lanes that are served at a time read eight rows.
+//
+// A weight p goes into the product as two bf16 terms, 16 bits of it (one term, 8 bits, would be as large an error as the result's own rounding; the third,
+// which attention of few rows has, is 2^-8 of an error that the rounding of bf16 results hides already).
+#pragma once
+#include "vt_attend_kernel.h"
+
+namespace vt {
+
+template <int DP, int HELD, int NT>
+__global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
+    constexpr int W = 4, E = DP / 16, KS = DP / 32, CH = DP / 8;      // CH: 16-byte places of a row in LDS
+    constexpr int TN = DP <= 128 ? 64 : 32, PIECES = TN / 16;
+    constexpr int PER = HELD == kHeld16 ? 8 : HELD == kHeld8 ? 16 : 32;      // values of a 16-byte load
+    constexpr int COLS = DP / PER, LOADS = (16 * COLS + 63) / 64;            // loads of a row; of a lane for 16 rows
+    constexpr int UNITS = 2 * PIECES / W;                                    // 16 rows of K or V that a wave brings
+    __shared__ __align__(16) u32x4 held[2][2][TN][CH];
+    __shared__ int flags[2][PIECES];      // 1: a page outside the cache, 2: NaN or infinities among the values
+
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const int h = blockIdx.x % a.cache.heads, block = a.row_blocks - 1 - blockIdx.x / a.cache.heads, b = blockIdx.y;      // (the longest first)
+    const int D = a.cache.D, shift = a.cache.page_shift;
+    int first;
+    const int rows = rows_of(a.row_start, b, a.n, a.max_rows, first), len = tokens_of(a.lengths[b], a.most);
+    const int x0 = block * 16 * NT * W, all = rows * a.G;
+    if (x0 >= all) return;
+    // tokens that any of the workgroup's rows sees: `end` and those before it but for the gap
+    const int x0_row = x0 / a.G, x0_head = x0 - x0_row * a.G;
+    const int lowest = last_position(len, rows, x0_row), highest = last_position(len, rows, (min(x0 + 16 * NT * W, all) - 1) / a.G);
+    const int end = max(highest + 1, 0), sinks16 = min(round16(a.sinks), round16(end));
+    const int gap = max((max(lowest - a.window + 1, 0) & ~15) - sinks16, 0), count = end - gap;
+    auto real = [&](int t) { return t >= sinks16 ? t + gap : t; };
+
+    // q's operand (its sign that of the scale, so that the largest score stays the largest when it is scaled), and what the lane's rows see
+    const float by = fabsf(a.scale_log2);
+    const unsigned turn = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    u32x4 q[NT][KS];
+    int from[NT], upto[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int x = 16 * (NT * wave + nt) + m, y = x0_head + min(x, all - x0 - 1), up = by_group(a, y);
+        const int64_t at = (first + (int64_t)x0_row + up) * a.q_stride + (h * a.G + y - up * a.G) * D;
+        upto[nt] = last_position(len, rows, x0_row + up);
+        from[nt] = upto[nt] - a.window + 1;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int d = 32 * s + 8 * g;
+            const u32x4 u = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + at + (d < D ? d : 0));
+            q[nt][s] = d < D && by != 0.0f ? u ^ turn : u32x4{0, 0, 0, 0};
+        }
+    }
+
+    // Page numbers of 64 pages, one in each lane
+    const int32_t *pages = a.page_table + (int64_t)b * a.table_pages;
+    const int last_page = max(end - 1, 0) >> shift;
+    int window = real(0) >> shift, ids = pages[min(window + lane, last_page)];
+    auto rows16 = [&](int t) -> int64_t {      // of the cache, or -1
+        if (t >= count) return -1;
+        const int token = real(t), p = token >> shift;
+        if (p >= window + 64) {
+            window = p;
+            ids = pages[min(p + lane, last_page)];
+        }
+        const int64_t row = row_of_page(__builtin_amdgcn_readlane(ids, p - window), a.cache.pages, a.cache.heads, h, shift);
+        return row < 0 ? -1 : row + (token & ((1 << shift) - 1));
+    };
+
+    // What the wave brings of a tile: unit u is piece (W u + wave) % PIECES of K (the first PIECES of the 2 PIECES) or V
+    constexpr int kBeyond = 1 << 30, BITS = HELD == kHeld16 ? 16 : HELD == kHeld8 ? 8 : 4;
+    u32x4 raw[LOADS];
+    unsigned scale[LOADS];
+    int there = 0;
+    auto bring = [&](int u, int t0) {
+        const int unit = W * u + wave, piece = unit % PIECES;
+        const bool is_v = unit >= PIECES;
+        const int64_t row = rows16(t0 + 16 * piece);
+        there = row >= 0;
+        const int row_bytes = D * BITS / 8;
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(is_v ? a.cache.v : a.cache.k) + (row < 0 ? 0 : row) * row_bytes, 0,
+                                                              row < 0 ? 0 : 16 * row_bytes, 0x00027000);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int id = 64 * j + lane, r = id / COLS, c = id % COLS;
+            const bool inside = r < 16 && c * PER < D;
+            raw[j] = __builtin_amdgcn_raw_buffer_load_b128(buffer, inside ? r * row_bytes + 16 * c : kBeyond, 0, 0);
+            if constexpr (HELD != kHeld16) {
+                const int groups = HELD == kHeld4 ? D / kScaleGroup : 1;
+                const uint8_t *const scales = is_v ? a.cache.v_scale : a.cache.k_scale;
+                const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(scales + (row < 0 ? 0 : scale_of_row(row, groups, 0, shift))), 0,
+                                                                  row < 0 ? 0 : ((groups - 1) << shift) + 16, 0x00027000);
+                scale[j] = __builtin_amdgcn_raw_buffer_load_b8(of, inside ? (HELD == kHeld4 ? c << shift : 0) + r : kBeyond, 0, 0);
+            }
+        }
+    };
+    // ... into LDS.  `edge`: some row does not see some token of the tile
+    auto keep = [&](int u, int buf, int t0, bool edge) {
+        const int unit = W * u + wave, piece = unit % PIECES;
+        const int is_v = unit >= PIECES;
+        unsigned odd = 0;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int id = 64 * j + lane, r = id / COLS, c = id % COLS;
+            if (16 * COLS % 64 != 0 && r >= 16) continue;
+            u32x4 out[PER / 8];
+            const unsigned s = HELD == kHeld16 ? 0 : scale[j] << 23;
+            if constexpr (HELD == kHeld16) {
+                out[0] = raw[j];
+            } else if constexpr (HELD == kHeld8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned w = raw[j][i];
+                    out[i / 2][2 * (i % 2)] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, __uint_as_float(s), false));
+                    out[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, __uint_as_float(s), true));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    unsigned f[4];
+                    eight_codes(raw[j][i], s, f);
+                    out[i] = u32x4{f[0], f[1], f[2], f[3]};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < PER / 8; ++i) {
+                if (edge && is_v) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) odd |= ((out[i][k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+                }
+                held[buf][is_v][16 * piece + r][(c * (PER / 8) + i) ^ (r & 7)] = out[i];
+            }
+        }
+        if (is_v) {
+            const int bits = (there || t0 + 16 * piece >= count ? 0 : 1) | (__any(odd != 0) ? 2 : 0);
+            if (lane == 0) flags[buf][piece] = bits;
+        }
+    };
+    auto edge_of = [&](int t0) {
+        bool edge = t0 + TN > count;
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) {
+            const int token = real(t0 + 16 * t);
+            edge |= (token < highest - a.window + 1 && token + 15 >= a.sinks) || token + 15 > lowest;
+        }
+        return edge;
+    };
+
+    f32x4a acc[NT][E];
+    float top[NT], total[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        top[nt] = kNone, total[nt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) acc[nt][i] = f32x4a{0, 0, 0, 0};
+    }
+
+    const float scale_by = by != 0.0f ? by : 1.0f;      // (then q is zeros)
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    // `middle` is between the products
+    auto tile = [&](int buf, int t0, bool edge, auto middle) {
+        f32x4a s[NT][PIECES];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int t = 0; t < PIECES; ++t) s[nt][t] = f32x4a{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int c = 0; c < KS; ++c) {
+#pragma unroll
+            for (int t = 0; t < PIECES; ++t) {
+                const u32x4 f = held[buf][0][16 * t + m][(4 * c + g) ^ (m & 7)];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) s[nt][t] = mfma(f, q[nt][c], s[nt][t]);
+            }
+        }
+        int bits = 0;
+#pragma unroll
+        for (int t = 0; t < PIECES; ++t) bits |= flags[buf][t] << 2 * t;
+        bits = __builtin_amdgcn_readfirstlane(bits);
+        constexpr int kOdd = 0xAA;
+        unsigned sees[NT];      // a bit for each of the lane's tokens
+        float base[NT], sum[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            f32x4a (&z)[PIECES] = s[nt];
+            sees[nt] = 0;
+            if (edge || bits != 0) {
+#pragma unroll
+                for (int j = 0; j < 4 * PIECES; ++j) {
+                    const int token = real(t0 + 16 * (j / 4)) + 4 * g + j % 4;
+                    const bool seen = (token >= from[nt] || token < a.sinks) && token <= upto[nt] && (bits >> 2 * (j / 4) & 1) == 0;
+                    z[j / 4][j % 4] = seen ? z[j / 4][j % 4] : kNone;
+                    sees[nt] |= seen ? 1u << j : 0u;
+                }
+            }
+            float most = top[nt];
+#pragma unroll
+            for (int j = 0; j < 4 * PIECES; ++j) most = fmaxf(most, z[j / 4][j % 4]);
+            most = row_max(most);
+            base[nt] = most == kNone ? 0.0f : most * scale_by;
+            const float fade = top[nt] == kNone ? 0.0f : __builtin_amdgcn_exp2f(top[nt] * scale_by - base[nt]);
+            if (t0 != 0 && __any(most > top[nt])) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[nt][i][r] *= fade;
+                }
+            }
+            top[nt] = most;
+            sum[nt] = total[nt] * fade;
+        }
+        middle();
+#pragma unroll
+        for (int t = 0; t < PIECES; t += 2) {
+            u32x4 p[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4a z = s[nt][t + j / 2];
+                    const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[2 * j % 4], scale_by, -base[nt]));
+                    const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[2 * j % 4 + 1], scale_by, -base[nt]));
+                    sum[nt] += w0 + w1;
+                    const unsigned u0 = __float_as_uint(w0), u1 = __float_as_uint(w1);
+                    p[nt][0][j] = __builtin_amdgcn_perm(u1, u0, 0x07060302);
+                    p[nt][1][j] = pack_bf16(w0 - __uint_as_float(u0 & 0xFFFF0000u), w1 - __uint_as_float(u1 & 0xFFFF0000u));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                u32x4 f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int r = 4 * g + m / 4, c = 2 * i + m % 4 / 2;
+                    auto *at = reinterpret_cast<__attribute__((address_space(3))) char *>(
+                                   (__attribute__((address_space(3))) u32x4 *)&held[buf][1][16 * (t + k) + r][c ^ (r & 7)]) + 8 * (m % 2);
+                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(at));
+                    const u32x2 u = __builtin_bit_cast(u32x2, v);
+                    f[2 * k] = u.x, f[2 * k + 1] = u.y;
+                }
+                if (bits & kOdd) {
+                    // NaN and infinities among values that some row does not see: taken out, and counted for the rows that see them
+                    u32x4 odd[3];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        unsigned clean = 0;
+                        odd[0][j] = odd[1][j] = odd[2][j] = 0;
+#pragma unroll
+                        for (int half = 0; half < 32; half += 16) {
+                            const unsigned u = (f[j] >> half) & 0xFFFFu, one = 0x3F80u << half;
+                            odd[0][j] |= (u & 0x7FFFu) > 0x7F80u ? one : 0u;
+                            odd[1][j] |= u == 0x7F80u ? one : 0u;
+                            odd[2][j] |= u == 0xFF80u ? one : 0u;
+                            clean |= (u & 0x7F80u) == 0x7F80u ? 0u : u << half;
+                        }
+                        f[j] = clean;
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        u32x4 seen;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            seen[j] = (sees[nt] >> (4 * t + 2 * j) & 1 ? 0x3F80u : 0u) | (sees[nt] >> (4 * t + 2 * j + 1) & 1 ? 0x3F800000u : 0u);
+                        const float add[3] = {__builtin_nanf(""), __builtin_inff(), -__builtin_inff()};
+#pragma unroll
+                        for (int kind = 0; kind < 3; ++kind) {
+                            const f32x4a n = mfma(odd[kind], seen, f32x4a{0, 0, 0, 0});
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) acc[nt][i][x] += n[x] > 0.0f ? add[kind] : 0.0f;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 1; e >= 0; --e) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) acc[nt][i] = mfma(f, p[nt][e], acc[nt][i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) total[nt] = sum[nt];
+    };
+
+    if (count > 0) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            bring(u, 0);
+            keep(u, 0, 0, edge_of(0));
+        }
+        __syncthreads();
+        for (int t0 = 0, buf = 0; t0 < count; t0 += TN, buf ^= 1) {
+            const bool more = t0 + TN < count, next_edge = edge_of(t0 + TN);
+            if (more) bring(0, t0 + TN);
+            tile(buf, t0, edge_of(t0), [&]() {
+                if (UNITS > 1 && more) {
+                    keep(0, buf ^ 1, t0 + TN, next_edge);
+                    bring(1, t0 + TN);
+                }
+            });
+            if (more) keep(UNITS - 1, buf ^ 1, t0 + TN, next_edge);
+            __syncthreads();
+        }
+    }
+
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int x = 16 * (NT * wave + nt) + m;
+        const float sum = row_sum(total[nt]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (x >= all - x0) continue;
+        const int y = x0_head + x, up = by_group(a, y);
+        const int64_t row = first + (int64_t)x0_row + up;
+        const int head = h * a.G + y - up * a.G;
+        if (g == 0 && a.lse != nullptr) a.lse[row * a.hq + head] = log_sum_exp(top[nt] * scale_by, sum);
+        uint16_t *const out = static_cast<uint16_t *>(a.out) + row * a.out_stride + head * D + 4 * g;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if (16 * i >= D) break;
+            float o[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = sum == 0.0f ? 0.0f : acc[nt][i][r] * inverse;
+            Bf16::store4(out + 16 * i, o);
+        }
+    }
+}
+
+template <int DP, int NT>
+hipError_t run_prompt(const AttendArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)(a.cache.heads * a.row_blocks), (unsigned)a.requests);
+    if (a.cache.four) prompt_kernel<DP, kHeld4, NT><<<grid, 256, 0, st>>>(a);
+    else if (a.cache.k_scale != nullptr) prompt_kernel<DP, kHeld8, NT><<<grid, 256, 0, st>>>(a);
+    else prompt_kernel<DP, kHeld16, NT><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace vt
