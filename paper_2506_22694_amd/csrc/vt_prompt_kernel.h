@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     constexpr int COLS = DP / PER, LOADS = (16 * COLS + 63) / 64;            // loads of a row; of a lane for 16 rows
     constexpr int UNITS = 2 * PIECES / W;                                    // 16 rows of K or V that a wave brings
     __shared__ __align__(16) u32x4 held[2][2][TN][CH];
-    __shared__ int flags[2][PIECES];      // 1: a page outside the cache, 2: NaN or infinities among the values
+    __shared__ __align__(16) int flags[2][4];      // of the pieces.  1: a page outside the cache, 2: NaN or infinities among the values
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int h = blockIdx.x % a.cache.heads, block = a.row_blocks - 1 - blockIdx.x / a.cache.heads, b = blockIdx.y;      // (the longest first)
@@ -79,12 +79,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     constexpr int kBeyond = 1 << 30, BITS = HELD == kHeld16 ? 16 : HELD == kHeld8 ? 8 : 4;
     u32x4 raw[LOADS];
     unsigned scale[LOADS];
-    int there = 0;
-    auto bring = [&](int u, int t0) {
+    int64_t row = -1;      // of the wave's piece (the same one of K and V where it brings both)
+    auto bring = [&](int u, int t0) __attribute__((always_inline)) {
         const int unit = W * u + wave, piece = unit % PIECES;
         const bool is_v = unit >= PIECES;
-        const int64_t row = rows16(t0 + 16 * piece);
-        there = row >= 0;
+        if (u == 0) row = rows16(t0 + 16 * piece);
         const int row_bytes = D * BITS / 8;
         const auto buffer = __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(is_v ? a.cache.v : a.cache.k) + (row < 0 ? 0 : row) * row_bytes, 0,
                                                               row < 0 ? 0 : 16 * row_bytes, 0x00027000);
@@ -103,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         }
     };
     // ... into LDS.  `edge`: some row does not see some token of the tile
-    auto keep = [&](int u, int buf, int t0, bool edge) {
+    auto keep = [&](int u, int buf, int t0, bool edge) __attribute__((always_inline)) {
         const int unit = W * u + wave, piece = unit % PIECES;
         const int is_v = unit >= PIECES;
         unsigned odd = 0;
@@ -133,6 +132,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 #pragma unroll
             for (int i = 0; i < PER / 8; ++i) {
                 if (edge && is_v) {
+                    if (t0 + 16 * piece + r >= count) out[i] = u32x4{0, 0, 0, 0};      // (past the end there may be anything)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) odd |= ((out[i][k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
                 }
@@ -140,18 +140,12 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
             }
         }
         if (is_v) {
-            const int bits = (there || t0 + 16 * piece >= count ? 0 : 1) | (__any(odd != 0) ? 2 : 0);
+            const int bits = (row >= 0 || t0 + 16 * piece >= count ? 0 : 1) | (__any(odd != 0) ? 2 : 0);
             if (lane == 0) flags[buf][piece] = bits;
         }
     };
     auto edge_of = [&](int t0) {
-        bool edge = t0 + TN > count;
-#pragma unroll
-        for (int t = 0; t < PIECES; ++t) {
-            const int token = real(t0 + 16 * t);
-            edge |= (token < highest - a.window + 1 && token + 15 >= a.sinks) || token + 15 > lowest;
-        }
-        return edge;
+        return t0 < highest - a.window + 1 - gap || t0 + TN > lowest + 1 - gap;
     };
 
     f32x4a acc[NT][E];
@@ -165,8 +159,53 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 
     const float scale_by = by != 0.0f ? by : 1.0f;      // (then q is zeros)
     typedef __attribute__((ext_vector_type(4))) short s16x4;
+    typedef __attribute__((address_space(3))) char Lds;
+    typedef __attribute__((address_space(3))) u32x4 LdsVector;
+    typedef __attribute__((address_space(3))) s16x4 LdsFour;
+    // where a lane reads: of K places 4 c + g of row m, of V column pairs 2 i + (m % 4) / 2 of row 4 g + m / 4; all else is a constant beside it
+    Lds *const lds = (Lds *)&held[0][0][0][0];
+    const Lds *k_at[2];
+    Lds *v_at[4];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) k_at[c] = lds + 16 * (m * CH + ((4 * c + g) ^ (m & 7)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * g + m / 4;
+        v_at[i] = lds + 16 * (r * CH + ((2 * i + m % 4 / 2) ^ (r & 7))) + 8 * (m % 2);
+    }
+    // NaN and infinities among values that some row sees and another one does not: added to those that see them, and taken out, as 0 * inf must not
+    // reach the others.  (Out of line, a token after the other: what no sound cache holds.)
+    auto take_out_odd = [&](int buf, int t0) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int t = 0; t < TN; ++t) {
+            const int token = real(t0 + (t & ~15)) + (t & 15);
+            const char *const row = reinterpret_cast<const char *>(held[buf][1][t]);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 16 * ((2 * i + g / 2) ^ (t & 7)) + 8 * (g % 2));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const unsigned bits = r % 2 ? u[r / 2] & 0xFFFF0000u : u[r / 2] << 16;
+                    const float odd = (bits & 0x7F800000u) == 0x7F800000u ? __uint_as_float(bits) : 0.0f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) acc[nt][i][r] += (token >= from[nt] || token < a.sinks) && token <= upto[nt] ? odd : 0.0f;
+                }
+            }
+        }
+        __syncthreads();
+        for (int at = threadIdx.x; at < TN * CH; at += 256) {
+            u32x4 &u = held[buf][1][at / CH][at % CH];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if ((u[k] & 0x7F80u) == 0x7F80u) u[k] &= 0xFFFF0000u;
+                if ((u[k] & 0x7F800000u) == 0x7F800000u) u[k] &= 0x0000FFFFu;
+            }
+        }
+        __syncthreads();
+    };
     // `middle` is between the products
-    auto tile = [&](int buf, int t0, bool edge, auto middle) {
+    auto tile = [&](int buf, int t0, bool edge, auto middle) __attribute__((always_inline)) {
+        const int shifted = buf * (2 * TN * CH * 16);
         f32x4a s[NT][PIECES];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -177,47 +216,47 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         for (int c = 0; c < KS; ++c) {
 #pragma unroll
             for (int t = 0; t < PIECES; ++t) {
-                const u32x4 f = held[buf][0][16 * t + m][(4 * c + g) ^ (m & 7)];
+                const u32x4 f = *reinterpret_cast<const LdsVector *>(k_at[c % 2] + shifted + 16 * (16 * t * CH + 8 * (c / 2)));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) s[nt][t] = mfma(f, q[nt][c], s[nt][t]);
             }
         }
-        int bits = 0;
-#pragma unroll
-        for (int t = 0; t < PIECES; ++t) bits |= flags[buf][t] << 2 * t;
+        const int4 said = *reinterpret_cast<const int4 *>(flags[buf]);
+        int bits = said.x | said.y << 2;
+        if constexpr (PIECES == 4) bits |= said.z << 4 | said.w << 6;
         bits = __builtin_amdgcn_readfirstlane(bits);
         constexpr int kOdd = 0xAA;
-        unsigned sees[NT];      // a bit for each of the lane's tokens
-        float base[NT], sum[NT];
+        float base[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             f32x4a (&z)[PIECES] = s[nt];
-            sees[nt] = 0;
             if (edge || bits != 0) {
 #pragma unroll
                 for (int j = 0; j < 4 * PIECES; ++j) {
                     const int token = real(t0 + 16 * (j / 4)) + 4 * g + j % 4;
                     const bool seen = (token >= from[nt] || token < a.sinks) && token <= upto[nt] && (bits >> 2 * (j / 4) & 1) == 0;
                     z[j / 4][j % 4] = seen ? z[j / 4][j % 4] : kNone;
-                    sees[nt] |= seen ? 1u << j : 0u;
                 }
             }
-            float most = top[nt];
+            // (a maximum that is left behind by no more than 2^kLag stays the base: weights of up to that are as exact, and little is rescaled)
+            constexpr float kLag = 8.0f;
+            float most = kNone;
 #pragma unroll
             for (int j = 0; j < 4 * PIECES; ++j) most = fmaxf(most, z[j / 4][j % 4]);
-            most = row_max(most);
-            base[nt] = most == kNone ? 0.0f : most * scale_by;
-            const float fade = top[nt] == kNone ? 0.0f : __builtin_amdgcn_exp2f(top[nt] * scale_by - base[nt]);
-            if (t0 != 0 && __any(most > top[nt])) {
+            most = row_max(most) * scale_by;
+            if (__any(most > top[nt] + kLag)) {
+                const float now = fmaxf(top[nt], most), fade = top[nt] == kNone ? 0.0f : __builtin_amdgcn_exp2f(top[nt] - now);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[nt][i][r] *= fade;
                 }
+                top[nt] = now;
+                total[nt] *= fade;
             }
-            top[nt] = most;
-            sum[nt] = total[nt] * fade;
+            base[nt] = top[nt] == kNone ? 0.0f : top[nt];
         }
+        if (bits & kOdd) take_out_odd(buf, t0);
         middle();
 #pragma unroll
         for (int t = 0; t < PIECES; t += 2) {
@@ -229,7 +268,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
                     const f32x4a z = s[nt][t + j / 2];
                     const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[2 * j % 4], scale_by, -base[nt]));
                     const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[2 * j % 4 + 1], scale_by, -base[nt]));
-                    sum[nt] += w0 + w1;
+                    total[nt] += w0 + w1;
                     const unsigned u0 = __float_as_uint(w0), u1 = __float_as_uint(w1);
                     p[nt][0][j] = __builtin_amdgcn_perm(u1, u0, 0x07060302);
                     p[nt][1][j] = pack_bf16(w0 - __uint_as_float(u0 & 0xFFFF0000u), w1 - __uint_as_float(u1 & 0xFFFF0000u));
@@ -240,44 +279,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
                 u32x4 f;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const int r = 4 * g + m / 4, c = 2 * i + m % 4 / 2;
-                    auto *at = reinterpret_cast<__attribute__((address_space(3))) char *>(
-                                   (__attribute__((address_space(3))) u32x4 *)&held[buf][1][16 * (t + k) + r][c ^ (r & 7)]) + 8 * (m % 2);
-                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(at));
+                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        reinterpret_cast<LdsFour *>(v_at[i % 4] + shifted + 16 * ((TN + 16 * (t + k)) * CH + 8 * (i / 4))));
                     const u32x2 u = __builtin_bit_cast(u32x2, v);
                     f[2 * k] = u.x, f[2 * k + 1] = u.y;
-                }
-                if (bits & kOdd) {
-                    // NaN and infinities among values that some row does not see: taken out, and counted for the rows that see them
-                    u32x4 odd[3];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        unsigned clean = 0;
-                        odd[0][j] = odd[1][j] = odd[2][j] = 0;
-#pragma unroll
-                        for (int half = 0; half < 32; half += 16) {
-                            const unsigned u = (f[j] >> half) & 0xFFFFu, one = 0x3F80u << half;
-                            odd[0][j] |= (u & 0x7FFFu) > 0x7F80u ? one : 0u;
-                            odd[1][j] |= u == 0x7F80u ? one : 0u;
-                            odd[2][j] |= u == 0xFF80u ? one : 0u;
-                            clean |= (u & 0x7F80u) == 0x7F80u ? 0u : u << half;
-                        }
-                        f[j] = clean;
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        u32x4 seen;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            seen[j] = (sees[nt] >> (4 * t + 2 * j) & 1 ? 0x3F80u : 0u) | (sees[nt] >> (4 * t + 2 * j + 1) & 1 ? 0x3F800000u : 0u);
-                        const float add[3] = {__builtin_nanf(""), __builtin_inff(), -__builtin_inff()};
-#pragma unroll
-                        for (int kind = 0; kind < 3; ++kind) {
-                            const f32x4a n = mfma(odd[kind], seen, f32x4a{0, 0, 0, 0});
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) acc[nt][i][x] += n[x] > 0.0f ? add[kind] : 0.0f;
-                        }
-                    }
                 }
 #pragma unroll
                 for (int e = 1; e >= 0; --e) {
@@ -286,8 +291,6 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
                 }
             }
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) total[nt] = sum[nt];
     };
 
     if (count > 0) {
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         const int y = x0_head + x, up = by_group(a, y);
         const int64_t row = first + (int64_t)x0_row + up;
         const int head = h * a.G + y - up * a.G;
-        if (g == 0 && a.lse != nullptr) a.lse[row * a.hq + head] = log_sum_exp(top[nt] * scale_by, sum);
+        if (g == 0 && a.lse != nullptr) a.lse[row * a.hq + head] = log_sum_exp(top[nt], sum);
         uint16_t *const out = static_cast<uint16_t *>(a.out) + row * a.out_stride + head * D + 4 * g;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
