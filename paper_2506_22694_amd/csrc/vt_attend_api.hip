@@ -74,6 +74,10 @@ struct Split {
 // (Levels of a few short requests have no more steps than places: there it is one step to a workgroup and one tile to a wave, whose loads have
 // nothing to hide behind.  Longer shares were not measured on them.)
 constexpr int64_t kAttendWorkgroups = 512, kAttendWorkgroupsOfOne = 256;
+// Over 4 bits a tile is a quarter of the bytes and as many instructions, so that a CU needs more waves to have as much under way: as many workgroups as
+// its registers hold for rows of one tile (48 ragged requests of up to 16384 tokens 72.6 us with 512, 64.9 with 768, 131001 tokens of one 47.5
+// with 256, 36.0 with 512; with 768 it is the join that gets longer), but for short shares, whose join costs what the waves gain (four tree levels).
+constexpr int64_t kAttendWorkgroupsOfFour = 768, kAttendWorkgroupsOfOneOfFour = 512;
 // Up to here a workgroup takes a request whole, without the second launch: 300 tokens of one request 6.6 us whole, 7.9 in shares, 512 tokens
 // 8.9 and 8.0.  Where there are many requests the workgroups are enough: of two requests' worth of tokens for each workgroup and no more
 // than kAttendWholeOfMany (8-bit cache, 64 requests of up to 1000 tokens, 512 workgroups: 19.5 us whole, 26.0 in shares; 16 requests, 128
@@ -83,7 +87,7 @@ constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 // Query rows of a kv head and request from which on a chunk goes through LDS, and workgroups from which on each has 128 of them and not 64.
 constexpr int64_t kPromptRows = 64, kPromptWorkgroups = 256;
 
-Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32) {
+Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four) {
     Split s;
     if (n < 0 || n >= kMaxRows || q_heads < 1 || q_heads > VT_MAX_ATTENTION_HEADS || kv_heads < 1 || q_heads % kv_heads != 0 || D < 16 || D > VT_MAX_HEAD_DIM ||
         requests < 0 || requests > VT_MAX_REQUESTS || max_rows < 1 || n > (int64_t)requests * max_rows || max_length < 0 || max_length > kMaxLength)
@@ -98,7 +102,9 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     s.whole = max_length <= (few > kAttendWhole ? few : kAttendWhole);
     int64_t places = requests;
     if (!s.whole) {
-        places = ((requests == 1 ? kAttendWorkgroupsOfOne : kAttendWorkgroups) + units - 1) / units;
+        const bool more = four && s.row_tiles == 1 && !f32;
+        const int64_t workgroups = requests == 1 ? (more ? kAttendWorkgroupsOfOneOfFour : kAttendWorkgroupsOfOne) : more ? kAttendWorkgroupsOfFour : kAttendWorkgroups;
+        places = (workgroups + units - 1) / units;
         if (places > steps * requests) places = steps * requests;
     }
     if (places * units > kMaxGrid || places > 65535) return s;
@@ -108,7 +114,7 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     const size_t entry = (D + 2) * sizeof(float);
     // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
     // larger with fewer rows.  (Fewer requests of the same lengths may be taken in shares where these are taken whole.)
-    const size_t most = 2 * (size_t)(kAttendWorkgroups * per + kv_heads * (rows + per));
+    const size_t most = 2 * (size_t)(kAttendWorkgroupsOfFour * per + kv_heads * (rows + per));
     s.most_bytes = max_length <= kAttendWhole ? 0 : round_up(most * entry + requests * sizeof(int4), 256);
     if (s.whole) return s;
     s.entries = (size_t)units * places * 2 * per;
@@ -131,7 +137,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
         const int64_t most = sinks + 15 + window + 15 + (positions != nullptr ? vt::kTail : max_rows);
         seen = most < max_length ? most : max_length;
         // (what the workspace's size is asked with)
-        if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32).ok) return VT_ERR_SHAPE;
+        if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32, cache->type == VT_E2M1).ok) return VT_ERR_SHAPE;
     }
     // rows of a chunk: tiles that many of them share
     const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
@@ -142,7 +148,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
         split.row_tiles = cache->head_dim > 128 || (chunk + 127) / 128 * cache->heads * n_requests < kPromptWorkgroups ? 1 : 2;
         split.row_blocks = (int)((chunk + 64 * split.row_tiles - 1) / (64 * split.row_tiles));
     } else {
-        split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32);
+        split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1);
     }
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
@@ -284,7 +290,7 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
 
 size_t vt_paged_attention_ws_bytes(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t n_requests, int32_t max_rows,
                                    int64_t max_length) {
-    return split_of(n, q_heads, kv_heads, head_dim, n_requests, max_rows, max_length, false).most_bytes;
+    return split_of(n, q_heads, kv_heads, head_dim, n_requests, max_rows, max_length, false, false).most_bytes;
 }
 
 int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache, const int32_t *page_table,

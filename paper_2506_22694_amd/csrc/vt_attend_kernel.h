@@ -77,10 +77,16 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 // Eight fp32 values (none -0) as the sum of three operands: the leading 8 bits of what is just below the value, those of what is just below the
 // rest, and the rest, which has 8.  (Below it by the last of its 24 bits; below an infinity are the largest finite ones.  0 is three zeros.)
-template <typename Terms>
+// Two terms: the rest is rounded, 2^-17 of the value at most, and is not zero either.
+template <int TERMS, typename Terms>
 __device__ __forceinline__ void split_terms(float (&v)[8], Terms &terms) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < TERMS; ++i) {
+        if (TERMS == 2 && i == 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) terms[1][j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+            break;
+        }
         unsigned u[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -194,6 +200,7 @@ template <int DP, int HELD, int NT, bool F32Q, bool WINDOW>
 __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, F32Q>())) void attend_kernel(AttendArgs a) {
     constexpr int W = kAttendWaves, E = DP / 16, KS = DP / 32, TERMS = F32Q ? 3 : 1;      // (of q)
     constexpr bool FP8 = HELD == kHeld8, FP4 = HELD == kHeld4;
+    constexpr int P_TERMS = FP4 && !F32Q ? 2 : 3;      // of the weights: over 4 bits the matrix and vector instructions are what there is too much of
     constexpr int KL = FP4 ? (DP + 127) / 128 : FP8 ? DP / 64 : DP / 32;      // loads of a token's row of K in a lane, of 16 bytes (FP4, DP = 64: of 8)
     constexpr int VR = FP4 ? (DP + 127) / 128 : FP8 ? DP / 64 : DP / 32;      // registers of a token's E values of V
     constexpr int BITS = FP4 ? 4 : FP8 ? 8 : 16;
@@ -440,7 +447,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
 
         // NaN and infinities among values that some row does not see: 0 * inf must not reach it.  They are taken out of V, and counted in products
         // of ones for each row that sees them, whose sums become what they would have.
-        unsigned p[NT][3][4], sees[NT][4];
+        unsigned p[NT][P_TERMS][4], sees[NT][4];
         auto take_out_odd = [&]() {
 #pragma unroll
             for (int r = 0; r < VR; ++r) {
@@ -522,7 +529,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
                             float x[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(q[nt][2 * c + j / 4][j % 4]);
-                            split_terms(x, terms[nt]);
+                            split_terms<3>(x, terms[nt]);
                         } else {
                             terms[nt][0] = q[nt][c];
                         }
@@ -640,7 +647,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
 #pragma unroll
                         for (int j = 0; j < 8; ++j) w[j] = scaled(w[j], (v_scale[j / 4] >> 8 * (j % 4)) & 0xFF);      // (0 stays, whatever is held)
                     }
-                    split_terms(w, p[nt]);
+                    split_terms<P_TERMS>(w, p[nt]);
                 }
                 if (ends) {
                     // what lies past the end may be anything, NaN too
@@ -675,7 +682,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
                     u32x4 f[VF];
                     operands(r, f);
 #pragma unroll
-                    for (int e = 2; e >= 0; --e) {
+                    for (int e = P_TERMS - 1; e >= 0; --e) {
 #pragma unroll
                         for (int i = 0; i < VF; ++i) {
 #pragma unroll

@@ -28,8 +28,9 @@ struct NormArgs {
     int hq, hk, D, rot, neighbours;
     const void *wq, *wk;        // null: no norm
     float eps;
-    float inverse_D;            // (set by the launch, this and the next: 1 / D; tokens that a workgroup takes at a time)
+    float inverse_D;            // (set by the launch, this and the next two: 1 / D; tokens that a workgroup takes at a time)
     int tokens_log2;
+    double inverse_D64;
     const float *table;         // null: no rotation
     int64_t table_rows;
     IndexArgs positions;

@@ -8,7 +8,7 @@
 //   out^T [d, row] = V^T p^T           V's operand: four tokens of one column in a lane, by the transposing read of LDS; p's operand is what the
 //                                      first product leaves in a lane, so the running maxima and sums are a lane's own
 //
-// 16 bytes c of token t lie at place c ^ (t & 7) of the token's row in LDS: the eight lanes that are served at a time read eight rows.
+// 16 bytes c of token t lie at place c ^ key(t) of the token's row in LDS, so that the sixteen lanes that read sixteen rows use all of its 64 banks.
 //
 // A weight p goes into the product as two bf16 terms, 16 bits of it (one term, 8 bits, would be as large an error as the result's own rounding; the third,
 // which attention of few rows has, is 2^-8 of an error that the rounding of bf16 results hides already).
@@ -24,7 +24,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     constexpr int PER = HELD == kHeld16 ? 8 : HELD == kHeld8 ? 16 : 32;      // values of a 16-byte load
     constexpr int COLS = DP / PER, LOADS = (16 * COLS + 63) / 64;            // loads of a row; of a lane for 16 rows
     constexpr int UNITS = 2 * PIECES / W;                                    // 16 rows of K or V that a wave brings
-    __shared__ __align__(16) u32x4 held[2][2][TN][CH];
+    __shared__ __align__(512) u32x4 held[2][2][TN][CH];
+    auto key = [](int t) { return CH >= 16 ? t & 15 : t >> 1 & 7; };
     __shared__ __align__(16) int flags[2][4];      // of the pieces.  1: a page outside the cache, 2: NaN or infinities among the values
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) odd |= ((out[i][k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
                 }
-                held[buf][is_v][16 * piece + r][(c * (PER / 8) + i) ^ (r & 7)] = out[i];
+                held[buf][is_v][16 * piece + r][(c * (PER / 8) + i) ^ key(r)] = out[i];
             }
         }
         if (is_v) {
@@ -162,17 +163,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     typedef __attribute__((address_space(3))) char Lds;
     typedef __attribute__((address_space(3))) u32x4 LdsVector;
     typedef __attribute__((address_space(3))) s16x4 LdsFour;
-    // where a lane reads: of K places 4 c + g of row m, of V column pairs 2 i + (m % 4) / 2 of row 4 g + m / 4; all else is a constant beside it
-    Lds *const lds = (Lds *)&held[0][0][0][0];
-    const Lds *k_at[2];
-    Lds *v_at[4];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) k_at[c] = lds + 16 * (m * CH + ((4 * c + g) ^ (m & 7)));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 4 * g + m / 4;
-        v_at[i] = lds + 16 * (r * CH + ((2 * i + m % 4 / 2) ^ (r & 7))) + 8 * (m % 2);
-    }
+    // where a lane reads: of K places 4 c + g of row m, of V column pairs 2 i + (m % 4) / 2 of row 4 g + m / 4.  Rows are aligned to their size, so that c
+    // and i are exclusive ors of a constant, and all else is a constant to add.
+    const unsigned lds = (unsigned)(size_t)(Lds *)&held[0][0][0][0];
+    const unsigned k_at = lds + 16 * (m * CH + (g ^ key(m))), v_at = lds + 16 * ((4 * g + m / 4) * CH + ((m % 4 / 2) ^ key(4 * g + m / 4))) + 8 * (m % 2);
     // NaN and infinities among values that some row sees and another one does not: added to those that see them, and taken out, as 0 * inf must not
     // reach the others.  (Out of line, a token after the other: what no sound cache holds.)
     auto take_out_odd = [&](int buf, int t0) __attribute__((always_inline)) {
@@ -182,7 +176,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
             const char *const row = reinterpret_cast<const char *>(held[buf][1][t]);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 16 * ((2 * i + g / 2) ^ (t & 7)) + 8 * (g % 2));
+                const u32x2 u = *reinterpret_cast<const u32x2 *>(row + 16 * ((2 * i + g / 2) ^ key(t)) + 8 * (g % 2));
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const unsigned bits = r % 2 ? u[r / 2] & 0xFFFF0000u : u[r / 2] << 16;
@@ -216,7 +210,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         for (int c = 0; c < KS; ++c) {
 #pragma unroll
             for (int t = 0; t < PIECES; ++t) {
-                const u32x4 f = *reinterpret_cast<const LdsVector *>(k_at[c % 2] + shifted + 16 * (16 * t * CH + 8 * (c / 2)));
+                const u32x4 f = *reinterpret_cast<const LdsVector *>((Lds *)(size_t)((k_at + shifted) ^ 64u * c) + 16 * 16 * t * CH);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) s[nt][t] = mfma(f, q[nt][c], s[nt][t]);
             }
@@ -280,7 +274,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        reinterpret_cast<LdsFour *>(v_at[i % 4] + shifted + 16 * ((TN + 16 * (t + k)) * CH + 8 * (i / 4))));
+                        reinterpret_cast<LdsFour *>((Lds *)(size_t)((v_at + shifted) ^ 32u * i) + 16 * (TN + 16 * (t + k)) * CH));
                     const u32x2 u = __builtin_bit_cast(u32x2, v);
                     f[2 * k] = u.x, f[2 * k + 1] = u.y;
                 }
