@@ -84,8 +84,11 @@ constexpr int64_t kAttendWorkgroupsOfFour = 768, kAttendWorkgroupsOfOneOfFour = 
 // workgroups: 13.2 and 11.2; 64 requests of up to 4000: 60.5 and 46.0).
 constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
-// Query rows of a kv head and request from which on a chunk goes through LDS, and workgroups from which on each has 128 of them and not 64.
-constexpr int64_t kPromptRows = 64, kPromptWorkgroups = 256;
+// Chunks: query rows of a kv head and request from more of which than these on, and steps of all workgroups of attend_kernel from which on, they go through LDS;
+// workgroups that their tokens are cut into shares for, of so many tiles at least.  (Window of 4096, bf16, 32 heads of 128 values over 8, attend_kernel and
+// this: one request of 32 rows 22.5 us and 25, of 64 28.6 and 31, of 128 42.8 and 37.5, of 512 109 and 73; eight of 16 39.8 and 46, of 128 140 and 117.
+// A chunk in one share, 512 rows of one request: 109 us.)
+constexpr int64_t kPromptRows = 64, kPromptSteps = 6 * 512, kPromptWorkgroups = 512, kPromptTiles = 6;
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four) {
     Split s;
@@ -114,11 +117,29 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     const size_t entry = (D + 2) * sizeof(float);
     // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
     // larger with fewer rows.  (Fewer requests of the same lengths may be taken in shares where these are taken whole.)
-    const size_t most = 2 * (size_t)(kAttendWorkgroupsOfFour * per + kv_heads * (rows + per));
+    size_t most = 2 * (size_t)(kAttendWorkgroupsOfFour * per + kv_heads * (rows + per));
+    if (rows > kPromptRows && most < (size_t)kPromptWorkgroups * (D > 128 ? 64 : 128)) most = (size_t)kPromptWorkgroups * (D > 128 ? 64 : 128);
     s.most_bytes = max_length <= kAttendWhole ? 0 : round_up(most * entry + requests * sizeof(int4), 256);
     if (s.whole) return s;
     s.entries = (size_t)units * places * 2 * per;
     s.bytes = s.entries * entry + requests * sizeof(int4);
+    return s;
+}
+
+Split split_of_prompt(int64_t rows, int64_t requests, int heads, int D, int64_t seen, int64_t max_length) {
+    Split s;
+    const int64_t tile = D <= 128 ? 64 : 32, tiles = (seen + tile - 1) / tile, most = max_length <= kAttendWhole || tiles < 2 * kPromptTiles ? 1 : tiles / kPromptTiles;
+    const int64_t two = (rows + 127) / 128 * heads * requests;
+    s.ok = true;
+    s.row_tiles = D > 128 || two * most < kPromptWorkgroups ? 1 : 2;
+    const int64_t per = 64 * s.row_tiles, blocks = (rows + per - 1) / per, units = blocks * heads * requests;
+    int64_t places = kPromptWorkgroups / units;      // (so no more than kPromptWorkgroups * per rows of partial results: split_of's most_bytes)
+    if (places > most) places = most;
+    s.row_blocks = (int)blocks;
+    s.places = places < 1 ? 1 : (int)places;
+    if (s.places == 1) return s;
+    s.entries = (size_t)(units * per * s.places);
+    s.bytes = s.entries * (D + 2) * sizeof(float);
     return s;
 }
 
@@ -141,15 +162,10 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     }
     // rows of a chunk: tiles that many of them share
     const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
-    const bool prompt = window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows;
-    Split split;
-    if (prompt) {
-        split.ok = true;
-        split.row_tiles = cache->head_dim > 128 || (chunk + 127) / 128 * cache->heads * n_requests < kPromptWorkgroups ? 1 : 2;
-        split.row_blocks = (int)((chunk + 64 * split.row_tiles - 1) / (64 * split.row_tiles));
-    } else {
-        split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1);
-    }
+    Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1);
+    const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
+                        (int64_t)split.row_blocks * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >= kPromptSteps;
+    if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
     if (n == 0 || n_requests == 0) return VT_OK;

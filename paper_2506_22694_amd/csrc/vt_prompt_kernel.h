@@ -17,6 +17,9 @@
 
 namespace vt {
 
+// Where the partial results of share z of the workgroup's rows begin, in blocks of its rows
+__device__ __forceinline__ int64_t prompt_part(const AttendArgs &a, int z) { return ((int64_t)z * a.requests + blockIdx.y) * (a.cache.heads * a.row_blocks) + blockIdx.x; }
+
 template <int DP, int HELD, int NT>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     constexpr int W = 4, E = DP / 16, KS = DP / 32, CH = DP / 8;      // CH: 16-byte places of a row in LDS
@@ -41,6 +44,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     const int end = max(highest + 1, 0), sinks16 = min(round16(a.sinks), round16(end));
     const int gap = max((max(lowest - a.window + 1, 0) & ~15) - sinks16, 0), count = end - gap;
     auto real = [&](int t) { return t >= sinks16 ? t + gap : t; };
+    // of those the workgroup's share, one of gridDim.z
+    const int share = (count + TN * (int)gridDim.z - 1) / (TN * (int)gridDim.z) * TN, begin = min((int)blockIdx.z * share, max(count, 0)), stop = min(begin + share, count);
 
     // q's operand (its sign that of the scale, so that the largest score stays the largest when it is scaled), and what the lane's rows see
     const float by = fabsf(a.scale_log2);
@@ -64,7 +69,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     // Page numbers of 64 pages, one in each lane
     const int32_t *pages = a.page_table + (int64_t)b * a.table_pages;
     const int last_page = max(end - 1, 0) >> shift;
-    int window = real(0) >> shift, ids = pages[min(window + lane, last_page)];
+    int window = real(begin) >> shift, ids = pages[min(window + lane, last_page)];
     auto rows16 = [&](int t) -> int64_t {      // of the cache, or -1
         if (t >= count) return -1;
         const int token = real(t), p = token >> shift;
@@ -78,10 +83,12 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 
     // What the wave brings of a tile: unit u is piece (W u + wave) % PIECES of K (the first PIECES of the 2 PIECES) or V
     constexpr int kBeyond = 1 << 30, BITS = HELD == kHeld16 ? 16 : HELD == kHeld8 ? 8 : 4;
-    u32x4 raw[LOADS];
-    unsigned scale[LOADS];
+    struct Raw {
+        u32x4 raw[LOADS];
+        unsigned scale[LOADS];
+    } next;
     int64_t row = -1;      // of the wave's piece (the same one of K and V where it brings both)
-    auto bring = [&](int u, int t0) __attribute__((always_inline)) {
+    auto bring = [&](int u, int t0, Raw &x) __attribute__((always_inline)) {
         const int unit = W * u + wave, piece = unit % PIECES;
         const bool is_v = unit >= PIECES;
         if (u == 0) row = rows16(t0 + 16 * piece);
@@ -92,18 +99,18 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         for (int j = 0; j < LOADS; ++j) {
             const int id = 64 * j + lane, r = id / COLS, c = id % COLS;
             const bool inside = r < 16 && c * PER < D;
-            raw[j] = __builtin_amdgcn_raw_buffer_load_b128(buffer, inside ? r * row_bytes + 16 * c : kBeyond, 0, 0);
+            x.raw[j] = __builtin_amdgcn_raw_buffer_load_b128(buffer, inside ? r * row_bytes + 16 * c : kBeyond, 0, 0);
             if constexpr (HELD != kHeld16) {
                 const int groups = HELD == kHeld4 ? D / kScaleGroup : 1;
                 const uint8_t *const scales = is_v ? a.cache.v_scale : a.cache.k_scale;
                 const auto of = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(scales + (row < 0 ? 0 : scale_of_row(row, groups, 0, shift))), 0,
                                                                   row < 0 ? 0 : ((groups - 1) << shift) + 16, 0x00027000);
-                scale[j] = __builtin_amdgcn_raw_buffer_load_b8(of, inside ? (HELD == kHeld4 ? c << shift : 0) + r : kBeyond, 0, 0);
+                x.scale[j] = __builtin_amdgcn_raw_buffer_load_b8(of, inside ? (HELD == kHeld4 ? c << shift : 0) + r : kBeyond, 0, 0);
             }
         }
     };
     // ... into LDS.  `edge`: some row does not see some token of the tile
-    auto keep = [&](int u, int buf, int t0, bool edge) __attribute__((always_inline)) {
+    auto keep = [&](int u, int buf, int t0, bool edge, const Raw &x) __attribute__((always_inline)) {
         const int unit = W * u + wave, piece = unit % PIECES;
         const int is_v = unit >= PIECES;
         unsigned odd = 0;
@@ -112,13 +119,13 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
             const int id = 64 * j + lane, r = id / COLS, c = id % COLS;
             if (16 * COLS % 64 != 0 && r >= 16) continue;
             u32x4 out[PER / 8];
-            const unsigned s = HELD == kHeld16 ? 0 : scale[j] << 23;
+            const unsigned s = HELD == kHeld16 ? 0 : x.scale[j] << 23;
             if constexpr (HELD == kHeld16) {
-                out[0] = raw[j];
+                out[0] = x.raw[j];
             } else if constexpr (HELD == kHeld8) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const unsigned w = raw[j][i];
+                    const unsigned w = x.raw[j][i];
                     out[i / 2][2 * (i % 2)] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, __uint_as_float(s), false));
                     out[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, __uint_as_float(s), true));
                 }
@@ -126,7 +133,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     unsigned f[4];
-                    eight_codes(raw[j][i], s, f);
+                    eight_codes(x.raw[j][i], s, f);
                     out[i] = u32x4{f[0], f[1], f[2], f[3]};
                 }
             }
@@ -287,23 +294,23 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         }
     };
 
-    if (count > 0) {
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            bring(u, 0);
-            keep(u, 0, 0, edge_of(0));
-        }
+    if (begin < stop) {
+        Raw first_k;
+        bring(0, begin, first_k);
+        if (UNITS > 1) bring(1, begin, next);
+        keep(0, 0, begin, edge_of(begin), first_k);
+        if (UNITS > 1) keep(1, 0, begin, edge_of(begin), next);
         __syncthreads();
-        for (int t0 = 0, buf = 0; t0 < count; t0 += TN, buf ^= 1) {
-            const bool more = t0 + TN < count, next_edge = edge_of(t0 + TN);
-            if (more) bring(0, t0 + TN);
+        for (int t0 = begin, buf = 0; t0 < stop; t0 += TN, buf ^= 1) {
+            const bool more = t0 + TN < stop, next_edge = edge_of(t0 + TN);
+            if (more) bring(0, t0 + TN, next);
             tile(buf, t0, edge_of(t0), [&]() {
                 if (UNITS > 1 && more) {
-                    keep(0, buf ^ 1, t0 + TN, next_edge);
-                    bring(1, t0 + TN);
+                    keep(0, buf ^ 1, t0 + TN, next_edge, next);
+                    bring(1, t0 + TN, next);
                 }
             });
-            if (more) keep(UNITS - 1, buf ^ 1, t0 + TN, next_edge);
+            if (more) keep(UNITS - 1, buf ^ 1, t0 + TN, next_edge, next);
             __syncthreads();
         }
     }
@@ -313,6 +320,17 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
         const int x = 16 * (NT * wave + nt) + m;
         const float sum = row_sum(total[nt]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (x >= all - x0) continue;
+        if (gridDim.z > 1) {
+            const int64_t part = prompt_part(a, blockIdx.z) * (16 * NT * W) + x;
+            if (g == 0) a.part_ms[part] = make_float2(top[nt], sum);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (16 * i >= D) break;
+                const float o[4] = {acc[nt][i][0], acc[nt][i][1], acc[nt][i][2], acc[nt][i][3]};
+                F32::store4(a.part_o + part * D + 16 * i + 4 * g, o);
+            }
+            continue;
+        }
         const int y = x0_head + x, up = by_group(a, y);
         const int64_t row = first + (int64_t)x0_row + up;
         const int head = h * a.G + y - up * a.G;
@@ -329,12 +347,52 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     }
 }
 
+// The shares of a row joined: each brought to the maximum of all; a share's sum of 0 has nothing of the row.  LV lanes take a row, a workgroup 256 / LV of
+// a block's ROWS (a block to a workgroup: 256 rows of 32 heads in eight shares 94 us, 50.5 so).
+template <int LV, int ROWS>
+__global__ __launch_bounds__(256) void prompt_join_kernel(AttendArgs a) {
+    constexpr int PER = 256 / LV, PARTS = ROWS / PER;
+    const int grid = a.cache.heads * a.row_blocks, block = blockIdx.x / PARTS, x_block = block % grid, b = block / grid;
+    const int h = x_block % a.cache.heads, x = blockIdx.x % PARTS * PER + threadIdx.x / LV, at = (a.row_blocks - 1 - x_block / a.cache.heads) * ROWS + x;
+    const int D = a.cache.D, d = 4 * (threadIdx.x % LV);
+    int first;
+    if (at >= rows_of(a.row_start, b, a.n, a.max_rows, first) * a.G) return;
+    auto index = [&](int z) { return (((int64_t)z * a.requests + b) * grid + x_block) * ROWS + x; };
+    float top = kNone, total = 0.0f, o[4] = {};
+#pragma unroll 8
+    for (int z = 0; z < a.places; ++z) {
+        const float2 part = a.part_ms[index(z)];
+        top = part.y == 0.0f ? top : fmaxf(top, part.x);
+    }
+#pragma unroll 8
+    for (int z = 0; z < a.places; ++z) {
+        const float2 part = a.part_ms[index(z)];
+        float u[4];
+        F32::load4(a.part_o + index(z) * D + (d < D ? d : 0), u);
+        const bool nothing = part.y == 0.0f;
+        const float f = __builtin_amdgcn_exp2f(part.x - top);
+        total += nothing ? 0.0f : part.y * f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += nothing ? 0.0f : u[j] * f;
+    }
+    if (d >= D) return;
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] *= inverse;
+    const int row = first + at / a.G, head = h * a.G + at % a.G;
+    Bf16::store4(static_cast<uint16_t *>(a.out) + (int64_t)row * a.out_stride + head * D + d, o);
+    if (d == 0 && a.lse != nullptr) a.lse[(int64_t)row * a.hq + head] = log_sum_exp(top, total);
+}
+
 template <int DP, int NT>
 hipError_t run_prompt(const AttendArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.cache.heads * a.row_blocks), (unsigned)a.requests);
+    const dim3 grid((unsigned)(a.cache.heads * a.row_blocks), (unsigned)a.requests, (unsigned)a.places);
     if (a.cache.four) prompt_kernel<DP, kHeld4, NT><<<grid, 256, 0, st>>>(a);
     else if (a.cache.k_scale != nullptr) prompt_kernel<DP, kHeld8, NT><<<grid, 256, 0, st>>>(a);
     else prompt_kernel<DP, kHeld16, NT><<<grid, 256, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.places == 1) return e;
+    prompt_join_kernel<DP / 4, 64 * NT><<<grid.x * grid.y * (64 * NT / (1024 / DP)), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

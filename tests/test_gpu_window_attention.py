@@ -84,6 +84,8 @@ def check(cache, table, lengths, q, starts, window, sinks, mask=None, positions=
     return out, lse
 
 
+# Chunks of enough work go through a kernel of their own: layouts of many kv heads reach it with few rows and tokens, heads of every kernel's size among them
+WIDE = [(128, 128, 64), (96, 48, 128), (224, 32, 96), (64, 64, 32), (64, 32, 256), (120, 40, 160)]
 LAYOUTS = [(4, 2, 64), (32, 8, 128), (7, 1, 128), (6, 3, 256), (20, 1, 96), (3, 3, 32), (5, 1, 160)]
 WINDOWS = [(1, 0), (15, 1), (16, 16), (17, 4), (64, 0), (100, 33), (128, 200), (1 << 30, 0), (1, 1 << 30)]
 
@@ -147,6 +149,30 @@ def test_chunks_of_prompts(hq, hk, D, held, dtype):
         check(*a, window, sinks)
 
 
+@pytest.mark.parametrize("hq,hk,D", WIDE)
+@pytest.mark.parametrize("held", CACHES)
+def test_chunks_of_many_heads(hq, hk, D, held):
+    g = _gen(hq + D)
+    for page, lengths, rows in ((16, [40, 1, 0, 200, 333, 130, 64, 500], [40, 1, 3, 77, 150, 0, 70, 130]), (64, [400, 390, 700, 70, 65], [200, 1, 97, 70, 100])):
+        a = case(g, held, BF16, hq, hk, D, page, lengths, rows=rows)
+        for window, sinks in ((1, 0), (7, 2), (16, 16), (33, 0), (100, 20), (129, 4), (1 << 30, 0), (3, 1 << 30)):
+            check(*a, window, sinks)
+        for scale in (0.0, -0.2):
+            check(*a, 100, 4, scale=scale)
+
+
+@pytest.mark.parametrize("held", CACHES)
+@pytest.mark.parametrize("hq,hk,D", [(16, 4, 128), (6, 2, 64), (5, 1, 256)])
+def test_chunks_in_shares(held, hq, hk, D):
+    """Long windows of few heads and rows: a chunk's tokens are cut into shares, some of them of no tokens."""
+    g = _gen(hq)
+    a = case(g, held, BF16, hq, hk, D, 64, [9000, 300, 0, 5003], rows=[130, 140, 2, 77])
+    for window, sinks in ((8000, 4), (5000, 700), (1 << 30, 0)):
+        out, lse = check(*a, window, sinks)
+        again = vt.paged_attention(a[3], *a[:3], row_start=a[4], max_rows=140, window=window, sinks=sinks, return_lse=True)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 @pytest.mark.parametrize("held", CACHES)
 @pytest.mark.parametrize("hq,hk,D", [(32, 8, 128), (14, 2, 64), (4, 4, 256), (9, 1, 128)])
 def test_longer_chunks(held, hq, hk, D):
@@ -169,14 +195,14 @@ def test_more_requests_than_shares(held, rows):
 
 
 @pytest.mark.parametrize("held", CACHES)
-@pytest.mark.parametrize("kind", ["token", "tree", "prompt"])
+@pytest.mark.parametrize("kind", ["token", "tree", "prompt", "wide"])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_what_no_row_sees_may_be_anything(held, kind, D):
     """Pages between the sinks and the windows are out of the cache, other places that no row sees hold NaN, infinities and any scale."""
     g = _gen(D)
-    hk, page = 2, 16
-    lengths, rows = [900, 45, 333, 0, 16], {"token": None, "tree": [3, 2, 5, 1, 2], "prompt": [200, 45, 9, 2, 16]}[kind]
-    cache, table, lengths, q, starts = case(g, held, BF16, 4, hk, D, page, lengths, rows=rows)
+    hk, page = 64 if kind == "wide" else 2, 16
+    lengths, rows = [900, 45, 333, 0, 16], {"token": None, "tree": [3, 2, 5, 1, 2]}.get(kind, [200, 45, 9, 2, 16])
+    cache, table, lengths, q, starts = case(g, held, BF16, 2 * hk, hk, D, page, lengths, rows=rows)
     mask = torch.full((q.shape[0],), -1, device="cuda") if kind == "tree" else None
     if mask is not None:
         mask[0] = ~(1 << 10)
@@ -216,10 +242,10 @@ def test_what_no_row_sees_may_be_anything(held, kind, D):
 
 @pytest.mark.parametrize("held", CACHES)
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("D", [64, 128, 256])
-def test_nan_and_infinities_reach_only_the_rows_that_see_them(held, dtype, D):
+@pytest.mark.parametrize("hk,D", [(2, 64), (2, 128), (2, 256), (512, 64), (300, 128), (200, 256), (500, 32)])
+def test_nan_and_infinities_reach_only_the_rows_that_see_them(held, dtype, hk, D):
     g = _gen(D)
-    cache, table, lengths, q, starts = case(g, held, dtype, 4, 2, D, 16, [150], rows=[100])
+    cache, table, lengths, q, starts = case(g, held, dtype, 2 * hk, hk, D, 16, [150], rows=[100])
 
     def spot(token):
         return table[0, token // 16].long(), token % 16
@@ -260,11 +286,11 @@ def test_rows_and_lengths_that_say_more_than_there_is():
     assert out[0].eq(7.0).all() and out[3].eq(7.0).all() and out[1].ne(7.0).any() and out[2].ne(7.0).any()
 
 
-@pytest.mark.parametrize("rows", [[3, 2], [130, 70]])
+@pytest.mark.parametrize("rows", [[3, 2], [130, 70], [290, 1200]])
 def test_rows_apart_in_place_and_on_another_stream(rows):
     g = _gen(12)
     cache, table, lengths, q, starts = case(g, BF16, BF16, 8, 2, 64, 16, [300, 4000], rows=rows)
-    kw = dict(row_start=starts, max_rows=max(rows), window=200, sinks=3)
+    kw = dict(row_start=starts, max_rows=max(rows), window=2000, sinks=3)
     want = vt.paged_attention(q, cache, table, lengths, **kw)
     wide = torch.zeros(sum(rows), 10 * 64, device="cuda", dtype=BF16)
     wide[:, 64:9 * 64] = q.flatten(1)
@@ -287,15 +313,16 @@ def test_a_cache_beyond_32_bits():
     vt.kv_cache_write(cache, k, v, cache.slots(table, torch.zeros(250, dtype=torch.int64, device="cuda"), torch.arange(250, device="cuda")))
     length = torch.tensor([250], dtype=torch.int32, device="cuda")
     check(cache, table, length, _randn(g, 1, 8, D).to(BF16), None, 100, 10)
-    check(cache, table, length, _randn(g, 200, 8, D).to(BF16), torch.tensor([0, 200], dtype=torch.int32, device="cuda"), 100, 10)
+    for hq in (8, 1000):
+        check(cache, table, length, _randn(g, 200, hq, D).to(BF16), torch.tensor([0, 200], dtype=torch.int32, device="cuda"), 100, 10)
 
 
-@pytest.mark.parametrize("rows", [[1, 1], [4, 2], [150, 90]])
+@pytest.mark.parametrize("rows", [[1, 1], [4, 2], [150, 90], [600, 90]])
 def test_captured_in_a_graph(rows):
     g = _gen(14)
-    cache, table, lengths, q, starts = case(g, E2M1, BF16, 8, 2, 64, 16, [2500, 410], rows=rows)
+    cache, table, lengths, q, starts = case(g, E2M1, BF16, 32, 8, 64, 16, [2500, 410], rows=rows)
     mask = torch.randint(-(1 << 62), 1 << 62, (sum(rows),), generator=g, device="cuda") if rows[0] == 4 else None
-    ws = vt.AttentionWorkspace(sum(rows), 8, 2, 64, 2, max(rows), 2500, "cuda")
+    ws = vt.AttentionWorkspace(sum(rows), 32, 8, 64, 2, max(rows), 2500, "cuda")
     out = torch.empty_like(q)
     call = lambda: vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=max(rows), tail_mask=mask, max_length=2500, ws=ws, out=out,      # noqa: E731
                                       window=1200, sinks=4)
@@ -318,7 +345,7 @@ def test_captured_in_a_graph(rows):
 def test_the_same_every_time():
     g = _gen(15)
     for rows in (None, [200, 100, 1]):
-        cache, table, lengths, q, starts = case(g, BF16, BF16, 16, 4, 128, 64, [3000, 700, 90], rows=rows)
+        cache, table, lengths, q, starts = case(g, BF16, BF16, 64, 16, 128, 64, [3000, 700, 90], rows=rows)
         kw = dict(row_start=starts, max_rows=200 if rows else None, window=1024, sinks=4, return_lse=True)
         want = vt.paged_attention(q, cache, table, lengths, **kw)
         for _ in range(5):
