@@ -80,14 +80,14 @@ __device__ __forceinline__ Angle angle_of(const NormArgs &a, const Lane &l, int6
     return t;
 }
 // x turned by +angle, or by -angle (SIGN = -1): the transpose, for gradients
-template <int SIGN, typename V>
-__device__ __forceinline__ void turn(V *x, const Angle &t, bool neighbours) {
-    V y[8];
+template <int SIGN>
+__device__ __forceinline__ void turn(float *x, const Angle &t, bool neighbours) {
+    float y[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const V s = SIGN < 0 ? -t.s[j] : t.s[j], c = t.c[j];
-        const V a = neighbours ? x[2 * j] : x[j], b = neighbours ? x[2 * j + 1] : x[4 + j];
-        const V ra = a * c - b * s, rb = b * c + a * s;
+        const float s = SIGN < 0 ? -t.s[j] : t.s[j];
+        const float a = neighbours ? x[2 * j] : x[j], b = neighbours ? x[2 * j + 1] : x[4 + j];
+        const float ra = a * t.c[j] - b * s, rb = b * t.c[j] + a * s;
         y[j] = ra, y[4 + j] = rb;
     }
 #pragma unroll
