@@ -6,8 +6,9 @@
 
 A level's nodes go into the cache behind the prompt, in the order they were drafted; each sees the prompt, its ancestors and
 itself, by a mask over the last 64 cached tokens.  Weights are random (there is no checkpoint here); dense products are torch's.
+The cache may be held in 8 or 4 bits; a layer may have a sliding window, with some first tokens that stay visible.
 
-    python examples/draft_round.py [--cache e4m3] [--prompt 2000]
+    python examples/draft_round.py [--cache e4m3 | e2m1] [--prompt 2000] [--window 512 --sinks 4]
 """
 import argparse
 import os
@@ -22,12 +23,14 @@ import paper_2506_22694_amd as vt  # noqa: E402
 class Drafter:
     """One decoder layer's attention and a trimmed head over `vocabulary` tokens, in bfloat16."""
 
-    def __init__(self, d=1024, q_heads=8, kv_heads=4, head_dim=128, vocabulary=32000, trimmed=8192, seed=0, device="cuda"):
+    def __init__(self, d=1024, q_heads=8, kv_heads=4, head_dim=128, vocabulary=32000, trimmed=8192, seed=0, device="cuda",
+                 window=None, sinks=0):
         g = torch.Generator(device=device).manual_seed(seed)
 
         def randn(*shape, std=1.0):
             return (torch.randn(shape, generator=g, device=device) * std).bfloat16()
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.window, self.sinks = window, sinks
         self.embedding = randn(vocabulary, d)
         self.qkv = randn(d, (q_heads + 2 * kv_heads) * head_dim, std=d ** -0.5)
         self.out = randn(q_heads * head_dim, d, std=(q_heads * head_dim) ** -0.5)
@@ -46,7 +49,8 @@ class Drafter:
         q, k, v = self.project(x)
         q = vt.qkv_to_cache(q, k, v, cache, slots, positions, self.rope, self.q_norm, self.k_norm)
         a = vt.paged_attention(q, cache, page_table, lengths, row_start=row_start, max_rows=None if row_start is None else tokens.numel(),
-                               tail_mask=tail_mask, max_length=max_length, ws=ws)
+                               tail_mask=tail_mask, max_length=max_length, ws=ws, window=self.window, sinks=self.sinks,
+                               positions=positions if tail_mask is not None and self.window is not None else None)
         return x + a.flatten(1) @ self.out
 
 
@@ -113,13 +117,16 @@ def draft_round(drafter, prompt, cache, page_table, depth=3, width=8, keep=32, m
 
 def main():
     p = argparse.ArgumentParser()
-    p.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
+    types = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "e2m1": torch.float4_e2m1fn_x2}
+    p.add_argument("--cache", choices=list(types), default="bf16")
     p.add_argument("--prompt", type=int, default=1000)
+    p.add_argument("--window", type=int)
+    p.add_argument("--sinks", type=int, default=0)
     a = p.parse_args()
-    drafter = Drafter()
+    drafter = Drafter(window=a.window, sinks=a.sinks)
     page = 64
     pages = -(-(a.prompt + 64) // page)
-    cache = vt.KVCache(pages, page, drafter.kv_heads, drafter.head_dim, torch.float8_e4m3fn if a.cache == "e4m3" else torch.bfloat16)
+    cache = vt.KVCache(pages, page, drafter.kv_heads, drafter.head_dim, types[a.cache])
     page_table = torch.randperm(pages, device="cuda").int()[None].contiguous()
     prompt = torch.randint(0, 32000, (a.prompt,), device="cuda")
     tree = draft_round(drafter, prompt, cache, page_table)
