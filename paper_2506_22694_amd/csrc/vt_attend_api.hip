@@ -82,6 +82,8 @@ constexpr int64_t kAttendWorkgroupsOfFour = 768, kAttendWorkgroupsOfOneOfFour = 
 // 8.9 and 8.0.  Where there are many requests the workgroups are enough: of two requests' worth of tokens for each workgroup and no more
 // than kAttendWholeOfMany (8-bit cache, 64 requests of up to 1000 tokens, 512 workgroups: 19.5 us whole, 26.0 in shares; 16 requests, 128
 // workgroups: 13.2 and 11.2; 64 requests of up to 4000: 60.5 and 46.0).
+// Short windows make requests alike: whole from three quarters of the workgroups there at a time on (64 requests of up to 8192 tokens, a window of 1024
+// in bf16 42.2 us whole, 49.0 in shares, in 4 bits 21.6 and 27.2; of 4096, which not all of them fill, 133 and 98).
 constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
 // Chunks: query rows of a kv head and request from more of which than these on, and steps of all workgroups of attend_kernel from which on, they go through LDS;
@@ -90,7 +92,8 @@ constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 // A chunk in one share, 512 rows of one request: 109 us.)
 constexpr int64_t kPromptRows = 64, kPromptSteps = 6 * 512, kPromptWorkgroups = 512, kPromptTiles = 6;
 
-Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four) {
+Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four,
+               bool windowed = false) {
     Split s;
     if (n < 0 || n >= kMaxRows || q_heads < 1 || q_heads > VT_MAX_ATTENTION_HEADS || kv_heads < 1 || q_heads % kv_heads != 0 || D < 16 || D > VT_MAX_HEAD_DIM ||
         requests < 0 || requests > VT_MAX_REQUESTS || max_rows < 1 || n > (int64_t)requests * max_rows || max_length < 0 || max_length > kMaxLength)
@@ -102,7 +105,9 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     s.row_tiles = vt::attend_row_tiles((int)rows, D, f32);
     const int64_t per = 16 * s.row_tiles, blocks = (rows + per - 1) / per, units = kv_heads * blocks;
     const int64_t few = 2 * units * requests < kAttendWholeOfMany ? 2 * units * requests : kAttendWholeOfMany;
-    s.whole = max_length <= (few > kAttendWhole ? few : kAttendWhole);
+    const int64_t rounds = (units * requests + kAttendWorkgroups - 1) / kAttendWorkgroups;
+    s.whole = max_length <= (few > kAttendWhole ? few : kAttendWhole) ||
+              (windowed && max_length <= kAttendWholeOfMany && units * requests * 4 >= rounds * kAttendWorkgroups * 3);
     int64_t places = requests;
     if (!s.whole) {
         const bool more = four && s.row_tiles == 1 && !f32;
@@ -162,7 +167,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     }
     // rows of a chunk: tiles that many of them share
     const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
-    Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1);
+    Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1, window > 0);
     const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
                         (int64_t)split.row_blocks * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >= kPromptSteps;
     if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
