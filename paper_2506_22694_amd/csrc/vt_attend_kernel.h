@@ -260,7 +260,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
         }
         const int RG = nrows * a.G - x0;      // query rows from x0 on
         if (RG <= 0 || take <= 0) continue;
-        const int t0 = at_step * kAttendStep, t1 = complete ? len : min(len, t0 + take * kAttendStep);
+        const int t0 = at_step * kAttendStep;
+        int t1 = complete ? len : min(len, t0 + take * kAttendStep);
+        // WINDOW: a block of a chunk's rows ends at its last one, and leaves out what lies between the sinks and the window of its first
+        int window_from = 0;
+        if constexpr (WINDOW) {
+            if (a.row_blocks > 1 && a.tail_mask == nullptr) {
+                t1 = min(t1, last_position(len + gap, nrows, x0_row + by_group(a, x0_head + min(RG, 16 * NT) - 1)) + 1 - gap);
+                window_from = last_position(len + gap, nrows, x0_row) - a.window + 1 - gap;
+            }
+        }
         const int64_t kept_at = (((int64_t)blockIdx.x * a.places + place) * 2 + (segment != 0)) * (16 * NT);
         float *const kept_o = a.part_o + kept_at * D;
         float2 *const kept_ms = a.part_ms + kept_at;
@@ -509,7 +518,12 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
             }
         };
 
-        int token = t0 + kAttendTile * wave;
+        // the next tile of the wave that holds a token of the window, or of the sinks
+        auto wanted = [&](int t) {
+            if (WINDOW && t >= sinks16 && t + kAttendTile <= window_from) t += ((window_from - kAttendTile - t) / (kAttendTile * W) + 1) * (kAttendTile * W);
+            return t;
+        };
+        int token = wanted(t0 + kAttendTile * wave);
         if (token < t1) {
             int64_t row[2] = {rows16(token), rows16(token + 16)};
             load_k(row);
@@ -563,7 +577,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, (attend_occupancy<DP, HELD, NT, 
                 }
 
                 // the next tile's keys are asked for once this one's are used up, its values likewise below
-                const int next = token + kAttendTile * W;
+                const int next = wanted(token + kAttendTile * W);
                 int64_t next_row[2] = {rows16(next), rows16(next + 16)};
                 if constexpr (!LEAN) load_k(next_row);
                 else load_v(row);
