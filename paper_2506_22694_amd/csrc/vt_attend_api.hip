@@ -87,10 +87,11 @@ constexpr int64_t kAttendWorkgroupsOfFour = 768, kAttendWorkgroupsOfOneOfFour = 
 constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
 // Chunks: query rows of a kv head and request from more of which than these on, and steps of all workgroups of attend_kernel from which on, they go through LDS;
-// workgroups that their tokens are cut into shares for, of so many tiles at least.  (Window of 4096, bf16, 32 heads of 128 values over 8, attend_kernel and
-// this: one request of 32 rows 22.5 us and 25, of 64 28.6 and 31, of 128 42.8 and 37.5, of 512 109 and 73; eight of 16 39.8 and 46, of 128 140 and 117.
-// A chunk in one share, 512 rows of one request: 109 us.)
-constexpr int64_t kPromptRows = 64, kPromptSteps = 6 * 512, kPromptWorkgroups = 512, kPromptTiles = 6;
+// workgroups that their tokens are cut into shares for, of so many tiles at least.  (bf16, 32 heads of 128 values over 8, attend_kernel and this: a window of
+// 4096, one request of 32 rows, 1056 steps, 22.5 us and 25, of 512 109 and 73, eight of 128 140 and 117; of 2000, one of 64, 1088 steps, 21.6 and 23.9, of 128, 2176
+// steps, 29.3 and 27.3; of 512, eight of 32, 1280 steps, 31.2 and 20.2.  Heads of 64 values, whose steps are of 64 query rows: of 512, one of 64 rows, 160 steps, 15.5
+// and 16.0, of 128, 384 steps, 19.5 and 16.0.  A chunk in one share, 512 rows of one request: 109 us.)
+constexpr int64_t kPromptRows = 64, kPromptSteps = 1200, kPromptStepsOf64 = 300, kPromptWorkgroups = 512, kPromptTiles = 6;
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four,
                bool windowed = false) {
@@ -169,7 +170,8 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
     Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1, window > 0);
     const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
-                        (int64_t)split.row_blocks * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >= kPromptSteps;
+                        (int64_t)split.row_blocks * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >=
+                            (cache->head_dim > 64 ? kPromptSteps : kPromptStepsOf64);
     if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;

@@ -15,7 +15,11 @@
 // Softmax statistics are kept per row in a lane, which is also the row of all of the lane's sums: rescaling needs no exchange.
 //
 // 8-bit caches: codes become bf16 (exactly) on their way, two for each conversion; scales are powers of two and go on the scores
-// and on p, where they are exact as well.
+// and on p, where they are exact as well.  4-bit ones have a scale for 32 values, which goes into the conversion: a lane's keys of a token are then
+// DP / 4 values side by side, and its values E of one token, of one group each.
+//
+// WINDOW: a row sees sinks and a window.  Tokens are counted without those between (Request::gap), everything goes by that number but a tile's page and what a
+// row sees of it.
 //
 // Values of 24 bits -- the weights p, and q of fp32 rows -- are sums of three of 8, so they are three operands each, and products are exact as
 // for bf16.  An infinity on the other side is still one after three products only if all three terms have the value's sign and none is
@@ -24,7 +28,8 @@
 // 8 bits 61 instead of 65, 16 nodes of 64 heads of 64 values 71 instead of 81.)
 //
 // 131001 tokens of one request, 8 kv heads of 128 values in bf16, 4 query heads each: 537 MB in 80 us, 6.7 TB/s, where a plain read of as much
-// takes 79; 224 vector and 32 matrix instructions a tile (8 bits: 317 and 32; 48 ragged requests 541 MB in 95 us, 5.7 TB/s).
+// takes 79; 224 vector and 32 matrix instructions a tile (8 bits: 317 and 32; 48 ragged requests 541 MB in 95 us, 5.7 TB/s).  4 bits: 143 MB in 34 us,
+// 48 ragged requests 292 MB in 60, 4.8 TB/s: 262 and 24 instructions a tile, which do not overlap on a SIMD, are what it takes.
 #pragma once
 #include "vt_values.h"
 
