@@ -80,12 +80,14 @@ size_t vt_qk_norm_rope_backward_ws_bytes(int64_t n, int32_t head_dim);
  *   k, v              [pages, heads, page_size, head_dim] of type VT_BF16, VT_E4M3 or
  *                     VT_E2M1 (4 bits each: value 2 i of a row in the lower half of its
  *                     byte i, 2 i + 1 in the upper)
- *   k_scale, v_scale  [pages, heads, page_size] exponents of the scales, VT_E4M3
- *                     only (else NULL): code c stands for c * 2^(scale - 127).  (255 has
- *                     no place in fp32 but for the least codes: what reads or sees such
- *                     a token may get infinities and NaN.)
- *                     VT_E2M1: [pages, heads, head_dim / 32, page_size], scales of the
- *                     values 32 j .. 32 j + 31 of every token (255: they are NaN)
+ *   k_scale, v_scale  exponents of the scales: code c stands for c * 2^(scale - 127).
+ *                     VT_BF16: NULL
+ *                     VT_E4M3: [pages, heads, page_size].  (255 has no place in fp32 but
+ *                     for the least codes: what reads or sees such a token may get
+ *                     infinities and NaN.)
+ *                     VT_E2M1: [pages, heads, head_dim / 32, page_size], that of the values
+ *                     32 j .. 32 j + 31 of every token.  (255: they are NaN; values from
+ *                     2^128 on, which writing never leaves, are infinite.)
  *   page_size         a power of two, 16 .. 65536
  *   head_dim          a multiple of 16 (VT_E2M1: of 32), <= VT_MAX_HEAD_DIM
  *
@@ -138,7 +140,8 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *   out[i, h, :] = sum_t exp(s[t] - lse) * v[t, g, :],   lse[i, h] = log sum_t exp(s[t])
  *
  * in fp32 (a weight times an 8-bit row's scale counts as less, or not at all, below
- * 2^-126).  A row that sees nothing (or whose scores are all -inf) has out = 0 and
+ * 2^-126; weights of bf16 rows over 4 bits, and of prompts' chunks, are held in 16 bits, off by
+ * 2^-17 of themselves at most).  A row that sees nothing (or whose scores are all -inf) has out = 0 and
  * lse = -inf.  What a row does not see does not reach it, NaN, infinities and any scale
  * included.
  *
