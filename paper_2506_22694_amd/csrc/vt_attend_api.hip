@@ -86,6 +86,13 @@ constexpr int64_t kAttendWorkgroupsOfFour = 768, kAttendWorkgroupsOfOneOfFour = 
 // in bf16 42.2 us whole, 49.0 in shares, in 4 bits 21.6 and 27.2; of 4096, which not all of them fill, 133 and 98).
 constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 
+// Over 4 bits and with a window, bytes of a value's row for each step and 16 query rows up to which workgroups have 16 query rows each (4 bits: counted as 8): twice
+// as many workgroups of half the registers, whose beginnings and ends are what the time goes to, though each tile is read and converted by each of them (32
+// heads of 128 values over 8, a window of 4096, 8 nodes of four requests: bf16 24.8 us with two tiles, 21.8 with one, 8 bits 23.7 and 18.6, 4 bits 22.9
+// and 19.4; of 32 requests 83 and 118, 62 and 75, 56 and 60; 28 heads of 64 values over 4, a window of 1024, of two 15.5 and 12.1; no window in 4 bits, of four
+// 27.8 and 23.4, of 32 77 and 85.  Between: bf16 of eight 34.9 and 37.0, 8 bits of 16 44.8 and 43.4).
+constexpr int64_t kAttendOneTile = 1100000, kAttendOneTileOf16Bits = 1000000;
+
 // Chunks: query rows of a kv head and request from more of which than these on, and steps of all workgroups of attend_kernel from which on, they go through LDS;
 // workgroups that their tokens are cut into shares for, of so many tiles at least.  (bf16, 32 heads of 128 values over 8, attend_kernel and this: a window of
 // 4096, one request of 32 rows, 1056 steps, 22.5 us and 25, of 512 109 and 73, eight of 128 140 and 117; of 2000, one of 64, 1088 steps, 21.6 and 23.9, of 128, 2176
@@ -93,7 +100,7 @@ constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 // and 16.0, of 128, 384 steps, 19.5 and 16.0.  A chunk in one share, 512 rows of one request: 109 us.)
 constexpr int64_t kPromptRows = 64, kPromptSteps = 1200, kPromptStepsOf64 = 300, kPromptWorkgroups = 512, kPromptTiles = 6;
 
-Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, bool four,
+Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, int cache_type,
                bool windowed = false) {
     Split s;
     if (n < 0 || n >= kMaxRows || q_heads < 1 || q_heads > VT_MAX_ATTENTION_HEADS || kv_heads < 1 || q_heads % kv_heads != 0 || D < 16 || D > VT_MAX_HEAD_DIM ||
@@ -104,6 +111,10 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     // (workgroups and threads of a launch, and all requests' steps, are 32-bit numbers)
     if (rows > kMaxGrid || (int64_t)requests * max_rows * q_heads > kMaxGrid || (steps + 1) * requests > kMaxLength) return s;
     s.row_tiles = vt::attend_row_tiles((int)rows, D, f32);
+    const int64_t most_per = 16 * s.row_tiles;
+    if ((cache_type == VT_E2M1 || windowed) && !f32 &&
+        kv_heads * ((rows + 15) / 16) * steps * requests * D * (cache_type == VT_BF16 ? 2 : 1) <= (cache_type == VT_BF16 ? kAttendOneTileOf16Bits : kAttendOneTile))
+        s.row_tiles = 1;
     const int64_t per = 16 * s.row_tiles, blocks = (rows + per - 1) / per, units = kv_heads * blocks;
     const int64_t few = 2 * units * requests < kAttendWholeOfMany ? 2 * units * requests : kAttendWholeOfMany;
     const int64_t rounds = (units * requests + kAttendWorkgroups - 1) / kAttendWorkgroups;
@@ -111,7 +122,7 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
               (windowed && max_length <= kAttendWholeOfMany && units * requests * 4 >= rounds * kAttendWorkgroups * 3);
     int64_t places = requests;
     if (!s.whole) {
-        const bool more = four && s.row_tiles == 1 && !f32;
+        const bool more = cache_type == VT_E2M1 && s.row_tiles == 1 && !f32;
         const int64_t workgroups = requests == 1 ? (more ? kAttendWorkgroupsOfOneOfFour : kAttendWorkgroupsOfOne) : more ? kAttendWorkgroupsOfFour : kAttendWorkgroups;
         places = (workgroups + units - 1) / units;
         if (places > steps * requests) places = steps * requests;
@@ -123,7 +134,7 @@ Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int ma
     const size_t entry = (D + 2) * sizeof(float);
     // Any call of up to these sizes: units * places are below workgroups + units, units * per below kv_heads * (rows + per), and per is no
     // larger with fewer rows.  (Fewer requests of the same lengths may be taken in shares where these are taken whole.)
-    size_t most = 2 * (size_t)(kAttendWorkgroupsOfFour * per + kv_heads * (rows + per));
+    size_t most = 2 * (size_t)(kAttendWorkgroupsOfFour * most_per + kv_heads * (rows + most_per));
     if (rows > kPromptRows && most < (size_t)kPromptWorkgroups * (D > 128 ? 64 : 128)) most = (size_t)kPromptWorkgroups * (D > 128 ? 64 : 128);
     s.most_bytes = max_length <= kAttendWhole ? 0 : round_up(most * entry + requests * sizeof(int4), 256);
     if (s.whole) return s;
@@ -149,6 +160,12 @@ Split split_of_prompt(int64_t rows, int64_t requests, int heads, int D, int64_t 
     return s;
 }
 
+// Blocks of attend_kernel's most rows that a chunk's are
+int64_t prompt_steps(int64_t rows, int D) {
+    const int64_t per = 16 * vt::attend_row_tiles((int)rows, D, false);
+    return (rows + per - 1) / per;
+}
+
 // Both calls' checks and launch; a window of 0: none.
 int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache, const int32_t *page_table,
               int32_t table_pages, const int32_t *lengths, int32_t n_requests, const int32_t *row_start, int32_t max_rows, const uint64_t *tail_mask,
@@ -164,13 +181,13 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
         const int64_t most = sinks + 15 + window + 15 + (positions != nullptr ? vt::kTail : max_rows);
         seen = most < max_length ? most : max_length;
         // (what the workspace's size is asked with)
-        if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32, cache->type == VT_E2M1).ok) return VT_ERR_SHAPE;
+        if (!split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, max_length, f32, cache->type).ok) return VT_ERR_SHAPE;
     }
     // rows of a chunk: tiles that many of them share
     const int64_t chunk = (int64_t)max_rows * (q_heads / cache->heads);
-    Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type == VT_E2M1, window > 0);
+    Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type, window > 0);
     const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
-                        (int64_t)split.row_blocks * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >=
+                        prompt_steps(chunk, cache->head_dim) * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >=
                             (cache->head_dim > 64 ? kPromptSteps : kPromptStepsOf64);
     if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
@@ -313,7 +330,7 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
 
 size_t vt_paged_attention_ws_bytes(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t n_requests, int32_t max_rows,
                                    int64_t max_length) {
-    return split_of(n, q_heads, kv_heads, head_dim, n_requests, max_rows, max_length, false, false).most_bytes;
+    return split_of(n, q_heads, kv_heads, head_dim, n_requests, max_rows, max_length, false, VT_BF16).most_bytes;
 }
 
 int vt_paged_attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache, const int32_t *page_table,
