@@ -93,12 +93,13 @@ constexpr int64_t kAttendWhole = 384, kAttendWholeOfMany = 1536;
 // 27.8 and 23.4, of 32 77 and 85.  Between: bf16 of eight 34.9 and 37.0, 8 bits of 16 44.8 and 43.4).
 constexpr int64_t kAttendOneTile = 1100000, kAttendOneTileOf16Bits = 1000000;
 
-// Chunks: query rows of a kv head and request from more of which than these on, and steps of all workgroups of attend_kernel from which on, they go through LDS;
-// workgroups that their tokens are cut into shares for, of so many tiles at least.  (bf16, 32 heads of 128 values over 8, attend_kernel and this: a window of
-// 4096, one request of 32 rows, 1056 steps, 22.5 us and 25, of 512 109 and 73, eight of 128 140 and 117; of 2000, one of 64, 1088 steps, 21.6 and 23.9, of 128, 2176
-// steps, 29.3 and 27.3; of 512, eight of 32, 1280 steps, 31.2 and 20.2.  Heads of 64 values, whose steps are of 64 query rows: of 512, one of 64 rows, 160 steps, 15.5
-// and 16.0, of 128, 384 steps, 19.5 and 16.0.  A chunk in one share, 512 rows of one request: 109 us.)
-constexpr int64_t kPromptRows = 64, kPromptSteps = 1200, kPromptStepsOf64 = 300, kPromptWorkgroups = 512, kPromptTiles = 6;
+// Chunks: query rows of a kv head and request from more of which than these on, and steps (of attend_kernel's most rows) from which on, they go through LDS;
+// workgroups that their tokens are cut into shares for, of so many tiles at least.  (32 heads of 128 values over 8, attend_kernel and this, bf16: eight of 32 rows
+// over a window of 512, 1280 steps, 18.6 us and 20.4, of 48, 1920 steps, 30.8 and 20.5; four of 24 over 2000, 1632 steps, 27.8 and 25.2; one of 512 over 4096 109
+// and 73, eight of 128 140 and 117.  8 bits, whose tiles are less to read again: two of 64 over 2000, 2176 steps, 24.9 and 28.9, eight of 64 over 512, 2560 steps,
+// 27.6 and 23.3.  28 heads of 64 values over 4, whose steps are of 64 query rows, bf16: two of 128 over 512, 672 steps, 13.8 and 16.1, one over 2000, 952 steps,
+// 21.9 and 20.4; 4 bits 14.9 and 19.5, 22.5 and 22.8.  A chunk in one share, 512 rows of one request: 109 us.)
+constexpr int64_t kPromptRows = 64, kPromptSteps = 2400, kPromptStepsOf16Bits = 1600, kPromptStepsOf64 = 700, kPromptWorkgroups = 512, kPromptTiles = 6;
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, int cache_type,
                bool windowed = false) {
@@ -188,7 +189,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type, window > 0);
     const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
                         prompt_steps(chunk, cache->head_dim) * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >=
-                            (cache->head_dim > 64 ? kPromptSteps : kPromptStepsOf64);
+                            (cache->head_dim <= 64 ? kPromptStepsOf64 : cache->type == VT_BF16 ? kPromptStepsOf16Bits : kPromptSteps);
     if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;
