@@ -82,6 +82,26 @@ def test_windows_need_no_more_than_the_workspace_of_a_call_without():
                 assert status == ALIGN, (requests, rows, hq, D, most, window, sinks, status)
 
 
+@pytest.mark.parametrize("held,scales", [(1, None), (2, A), (4, A)])
+def test_any_split_of_any_cache_fits_the_workspace(held, scales):
+    rng = random.Random(held)
+    lib_ = vt.load_library()
+    for _ in range(600):
+        requests, rows, hk = rng.choice([1, 2, 5, 17, 64]), rng.choice([1, 2, 8, 17, 40, 130]), rng.choice([1, 2, 4, 8, 32])
+        hq, D, most = hk * rng.choice([1, 2, 4, 7]), rng.choice([32, 64, 96, 128, 160, 256]), rng.choice([385, 520, 1000, 5000, 20000, 131072])
+        n = requests * rows
+        size = lib_.vt_paged_attention_ws_bytes(n, hq, hk, D, requests, rows, most)
+        c = _cache(type=held, heads=hk, head_dim=D, k_scale=scales, v_scale=scales)
+        for less in (1, 2, 7):      # (of a workspace for more rows or longer requests than there are)
+            for window in (0, 100, 1000, 4096, 1 << 30):
+                m, length = max(1, rows // less), most // less
+                for mask in (None, A):
+                    status = lib_.vt_paged_attention_window(A, hq * D, 1, requests * m, hq, ctypes.addressof(c), A, 9000, A, requests, A, m, mask, None, 0, window, 4 if window else 0,
+                                                            length, 0.1, A, hq * D, 0x10002, A, size, None) if window else \
+                        lib_.vt_paged_attention(A, hq * D, 1, requests * m, hq, ctypes.addressof(c), A, 9000, A, requests, A, m, mask, length, 0.1, A, hq * D, 0x10002, A, size, None)
+                    assert status == ALIGN, (requests, m, hq, hk, D, length, window, mask, status)
+
+
 def test_python_refuses_before_anything_is_sent():
     q = torch.ones(1, 2, 64)
     with pytest.raises(ValueError):

@@ -138,6 +138,27 @@ def test_tree_levels(hq, hk, D, rows, held, dtype):
             check(*a, window, sinks, mask=mask)
 
 
+@pytest.mark.parametrize("hq,hk,D,rows", [(32, 8, 128, 8), (20, 4, 96, 5), (64, 32, 64, 9), (28, 4, 64, 16), (28, 4, 64, 40)])
+@pytest.mark.parametrize("held", CACHES)
+def test_levels_of_many_requests(hq, hk, D, rows, held):
+    """As much to read that workgroups have two or four tiles of query rows."""
+    g = _gen(hq + D + rows)
+    n = 40
+    lengths = [3500] + [[64, 1, 700, 63, 0, 130, 333][i % 7] for i in range(n - 2)] + [3073]
+    counts = [[rows, 1, 0, 3, 2][i % 5] for i in range(n)]
+    a = case(g, held, BF16, hq, hk, D, 32, lengths, rows=counts)
+    mask = torch.randint(-(1 << 63), (1 << 63) - 1, (sum(counts),), generator=g, device="cuda")
+    mask[0], mask[1], mask[-1] = 0, -1, -(1 << 63)
+    base = torch.repeat_interleave(a[2].long(), torch.tensor(counts, device="cuda"))
+    positions = base - 40 + torch.randint(-30, 50, (sum(counts),), generator=g, device="cuda")
+    for window, sinks in ((3000, 20), (100, 3000), (1 << 30, 0)):
+        check(*a, window, sinks, mask=mask, positions=positions, max_length=1 << 16)
+        check(*a, window, sinks, mask=mask, max_length=1 << 16)
+    check(*a, 3000, 4, max_length=1 << 16)
+    if held == E2M1:
+        four._check_attention(*a, mask=mask, max_length=1 << 16)
+
+
 @pytest.mark.parametrize("hq,hk,D", LAYOUTS)
 @pytest.mark.parametrize("held", CACHES)
 @pytest.mark.parametrize("dtype", [BF16, F32])
