@@ -262,6 +262,40 @@ def test_what_no_row_sees_may_be_anything(held, kind, D):
 
 
 @pytest.mark.parametrize("held", CACHES)
+@pytest.mark.parametrize("hq,D", [(16, 64), (8, 64), (16, 128)])
+def test_hidden_nan_and_infinities_reach_only_the_rows_that_see_them(held, hq, D):
+    """Five nodes whose heads fill two or four tiles (requests may be long)."""
+    g = _gen(hq + D)
+    cache, table, lengths, q, starts = case(g, held, BF16, hq, 2, D, 16, [100], rows=[5])
+    for token, value in ((80, math.inf), (90, math.nan)):
+        page, place = table[0, token // 16].long(), token % 16
+        if held == BF16:
+            cache.v[page, 1, place, token % 17] = value
+        elif held == E4M3:
+            cache.v.view(torch.uint8)[page, 1, place, token % 17] = 0x7F
+        else:
+            cache.v_scale[page, 1, token // 10 % (D // 32), place] = 255
+    page, place = table[0, 85 // 16].long(), 85 % 16
+    if held == E2M1:
+        cache.k_scale[page, 0, 0, place] = 255
+    elif held == E4M3:
+        cache.k.view(torch.uint8)[page, 0, place, 3] = 0x7F
+    else:
+        cache.k[page, 0, place, 3] = math.nan
+    hidden = (1 << 64) - 1
+    for token in (80, 85, 90):
+        hidden &= ~(1 << (token - 100 + 64))
+    masks = [hidden | 1 << (80 - 36), hidden, hidden | 1 << (90 - 36), hidden | 1 << (85 - 36), hidden]
+    mask = torch.tensor([m - (1 << 64) if m >> 63 else m for m in masks], device="cuda")
+    for kw in ({}, {"max_length": 1 << 22}):
+        out, lse = check(cache, table, lengths, q, starts, 1 << 29, 0, mask=mask, **kw)
+        assert out[1].isfinite().all() and out[4].isfinite().all() and lse[1].isfinite().all()
+        assert not out[0].isfinite().all() and not out[2].isfinite().all() and lse[3].isnan().any()
+        if held == E2M1:
+            four._check_attention(cache, table, lengths, q, starts, mask=mask, **kw)
+
+
+@pytest.mark.parametrize("held", CACHES)
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("hk,D", [(2, 64), (2, 128), (2, 256), (512, 64), (300, 128), (200, 256), (500, 32)])
 def test_nan_and_infinities_reach_only_the_rows_that_see_them(held, dtype, hk, D):
