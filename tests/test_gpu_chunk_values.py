@@ -1,0 +1,92 @@
+"""Chunks of prompts over values where sums of bf16 terms can go wrong: infinities that every row sees, several tiles inside the window, met with weights
+whose lower bits are zero.  Against 64 bits by the definition, with the tolerances of test_gpu_window_attention.py."""
+import math
+
+import pytest
+import torch
+
+import paper_2506_22694_amd as vt
+from test_gpu_attention import BF16, _gen
+from test_gpu_four_bits import E2M1
+from test_gpu_window_attention import WIDE, case, check
+
+pytestmark = pytest.mark.gpu
+
+
+def hold(cache, table, token, head, d, value, b=0):
+    """An infinity (4 bits: a group of zeros beside it, 6 or -6 at a scale of 2^127) or NaN as value d of a token's row."""
+    page, place = table[b, token // cache.page_size].long(), token % cache.page_size
+    if cache.v.dtype == BF16:
+        cache.v[page, head, place, d] = value
+        return
+    codes = cache.v.view(torch.uint8)[page, head, place]
+    group = d // 32
+    codes[16 * group:16 * group + 16] = 0
+    codes[d // 2] = (0xF if value < 0 else 7) << 4 * (d % 2)
+    cache.v_scale[page, head, group, place] = 255 if math.isnan(value) else 254
+
+
+@pytest.mark.parametrize("held", [BF16, E2M1])
+@pytest.mark.parametrize("hq,hk,D", WIDE)
+def test_infinities_that_every_row_sees(held, hq, hk, D):
+    """Rows of q = 0 have weights of 1, of which bf16 holds all; other rows a token of weight 1 where the largest score's is."""
+    g = _gen(hq + D)
+    cache, table, lengths, q, starts = case(g, held, BF16, hq, hk, D, 16, [700, 640], rows=[130, 100])
+    q[::3] = 0.0
+    hold(cache, table, 200, 0, 5, math.inf)
+    hold(cache, table, 350, 1, D - 3, -math.inf)
+    hold(cache, table, 330, hk - 1, 9, math.nan)
+    hold(cache, table, 223, 2, 1, math.inf, 1)
+    hold(cache, table, 222, 2, 1, math.inf, 1)
+    if held == BF16:      # the largest score of a row of each kv head
+        cache.k[table[0, 350 // 16].long(), :, 350 % 16] = 2.0 * q[1].view(hk, -1, D)[:, 0]
+    for window, sinks in ((600, 0), (500, 40), (1 << 30, 0)):
+        out, lse = check(cache, table, lengths, q, starts, window, sinks)
+        G = hq // hk
+        assert out[:130, :G, 5].eq(math.inf).all() and out[:130, G:2 * G, D - 3].eq(-math.inf).all() and out[130:, 2 * G:3 * G, 1].eq(math.inf).all()
+        assert out[:130, -G:, 9].isnan().all() and lse.isfinite().all()
+
+
+@pytest.mark.parametrize("held", [BF16, E2M1])
+@pytest.mark.parametrize("hq,hk,D", [(16, 4, 128), (6, 2, 64), (5, 1, 256)])
+def test_infinities_in_a_share_of_a_chunk(held, hq, hk, D):
+    g = _gen(hq)
+    cache, table, lengths, q, starts = case(g, held, BF16, hq, hk, D, 64, [9000, 5003], rows=[130, 77])
+    q[::2] = 0.0
+    hold(cache, table, 4000, 0, 5, math.inf)
+    hold(cache, table, 2500, hk - 1, 6, -math.inf, 1)
+    for window, sinks in ((8000, 4), (5000, 700), (1 << 30, 0)):
+        out, _ = check(cache, table, lengths, q, starts, window, sinks)
+        if window >= 8000:
+            assert out[:130, :hq // hk, 5].eq(math.inf).all() and out[130:, -(hq // hk):, 6].eq(-math.inf).all()
+
+
+@pytest.mark.parametrize("held", [BF16, E2M1])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows", [2, 130])      # (few rows and chunks have a kernel each)
+def test_infinities_of_small_weights(held, D, rows):
+    """Weights that are powers of two, down to 2^-100 of the row's largest: scores are whole numbers times log 2."""
+    g = _gen(D)
+    hk = 96
+    cache, table, lengths, q, starts = case(g, held, BF16, hk, hk, D, 16, [700], rows=[rows])
+    assert float(torch.tensor(math.log(2.0), dtype=torch.float32) * torch.tensor(1.4426950408889634, dtype=torch.float32)) == 1.0
+    q.zero_()
+    q[..., 0] = -1.0
+    (cache.k.view(torch.uint8) if held == E2M1 else cache.k).zero_()
+    exponents = torch.tensor([0, 1, 2, 23, 24, 60, 96], device="cuda")
+    page, place = table[0, 200 // 16].long(), 200 % 16
+    for head in range(hk):
+        e = int(exponents[head % 7])
+        if held == BF16:
+            cache.k[page, head, place, 0] = float(e)
+        elif e:      # 1, 2, 3 * 2^3, ...: a magnitude of the codes times a power of two
+            e = {23: 24}.get(e, e)
+            m = max(i for i, x in enumerate((0, 0.5, 1, 1.5, 2, 3, 4, 6)) if x and math.log2(e / x) % 1 == 0) if e != 60 else 0
+            if e == 60:
+                e, m = 64, 6
+            size = (0, 0.5, 1, 1.5, 2, 3, 4, 6)[m]
+            cache.k.view(torch.uint8)[page, head, place, 0] = m
+            cache.k_scale[page, head, 0, place] = 127 + int(math.log2(e / size))
+        hold(cache, table, 200, head, 7, math.inf)
+    out, lse = check(cache, table, lengths, q, starts, 600, 0, scale=math.log(2.0))
+    assert out[:, :, 7].eq(math.inf).all() and lse.isfinite().all()
