@@ -177,12 +177,21 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
     // and i are exclusive ors of a constant, and all else is a constant to add.
     const unsigned lds = (unsigned)(size_t)(Lds *)&held[0][0][0][0];
     const unsigned k_at = lds + 16 * (m * CH + (g ^ key(m))), v_at = lds + 16 * ((4 * g + m / 4) * CH + ((m % 4 / 2) ^ key(4 * g + m / 4))) + 8 * (m % 2);
-    // NaN and infinities among values that some row sees and another one does not: added to those that see them, and taken out, as 0 * inf must not
-    // reach the others.  (Out of line, a token after the other: what no sound cache holds.)
-    auto take_out_odd = [&](int buf, int t0) __attribute__((always_inline)) {
+    // NaN and infinities among values that some row sees and another one does not: added to those that see them (at scores above -inf, as attend_kernel does), and
+    // taken out, as 0 * inf must not reach the others.  (Out of line, a token after the other: what no sound cache holds.)
+    auto take_out_odd = [&](int buf, const f32x4a (&z)[NT][PIECES]) __attribute__((always_inline)) {
+        unsigned sees[NT] = {};      // bit 4 t + i: of token 16 t + 4 g + i
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int j = 4 * PIECES - 1; j >= 0; --j) sees[nt] = 2 * sees[nt] + (z[nt][j / 4][j % 4] > kNone ? 1u : 0u);
+        }
 #pragma unroll 1
         for (int t = 0; t < TN; ++t) {
-            const int token = real(t0 + (t & ~15)) + (t & 15);
+            bool seen[NT];      // by the lane's row
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+                seen[nt] = ((unsigned)__builtin_amdgcn_ds_bpermute(4 * ((t & 12) * 4 + m), (int)sees[nt]) >> (4 * (t >> 4) + (t & 3)) & 1) != 0;
             const char *const row = reinterpret_cast<const char *>(held[buf][1][t]);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
                     const unsigned bits = r % 2 ? u[r / 2] & 0xFFFF0000u : u[r / 2] << 16;
                     const float odd = (bits & 0x7F800000u) == 0x7F800000u ? __uint_as_float(bits) : 0.0f;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) acc[nt][i][r] += (token >= from[nt] || token < a.sinks) && token <= upto[nt] ? odd : 0.0f;
+                    for (int nt = 0; nt < NT; ++nt) acc[nt][i][r] += seen[nt] ? odd : 0.0f;
                 }
             }
         }
@@ -260,8 +269,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
             }
             base[nt] = top[nt] == kNone ? 0.0f : top[nt];
         }
-        if (bits & kOdd) take_out_odd(buf, t0);
         middle();
+        // (here and unlikely, for the order that the products' code gets: 8192 rows 588 us and chunks of 64-value heads 134.6, ahead of `middle` 608 and 145)
+        if (__builtin_expect((bits & kOdd) != 0, 0)) take_out_odd(buf, s);
 #pragma unroll
         for (int t = 0; t < PIECES; t += 2) {
             u32x4 p[NT][2];

@@ -90,3 +90,23 @@ def test_infinities_of_small_weights(held, D, rows):
         hold(cache, table, 200, head, 7, math.inf)
     out, lse = check(cache, table, lengths, q, starts, 600, 0, scale=math.log(2.0))
     assert out[:, :, 7].eq(math.inf).all() and lse.isfinite().all()
+
+
+@pytest.mark.parametrize("hq,hk,D", WIDE)
+@pytest.mark.parametrize("rows", [2, 130])
+def test_infinities_at_scores_of_minus_infinity_beside_a_window(hq, hk, D, rows):
+    """Where a window begins or ends, a token of weight 0 is as one that is not seen: in a chunk as in few rows."""
+    g = _gen(D)
+    cache, table, lengths, q, starts = case(g, BF16, BF16, hq, hk, D, 16, [700], rows=[rows])
+    q = q.abs()
+    out = []
+    for value in (math.inf, -math.inf, math.nan, 0.0):
+        for token in (670, 690) if rows == 2 else (580, 600, 633, 690):
+            page, place = table[0, token // 16].long(), token % 16
+            cache.k[page, :, place] = -math.inf
+            cache.v[page, :, place, token % 7] = value
+        out.append(vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=rows, window=40, return_lse=True))
+    whole = q.ne(0).all(-1)      # (0 * -inf is NaN: a query with a zero in it, one of millions, has a score of NaN)
+    for got in out[:-1]:
+        assert torch.equal(got[0][whole], out[-1][0][whole]) and torch.equal(got[1][whole], out[-1][1][whole])
+    assert out[-1][0][whole].isfinite().all() and out[-1][1][whole].isfinite().all() and whole.sum() > 0.99 * whole.numel()
