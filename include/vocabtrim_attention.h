@@ -141,9 +141,11 @@ int vt_kv_cache_read(const vt_kv_cache *cache, const void *slots, int slot_type,
  *
  * in fp32 (a weight times an 8-bit row's scale counts as less, or not at all, below
  * 2^-126; weights of bf16 rows over 4 bits, and of prompts' chunks, are held in 16 bits, off by
- * 2^-17 of themselves at most).  A row that sees nothing (or whose scores are all -inf) has out = 0 and
+ * 2^-16 of themselves at most; chunks have 8-bit values as bf16, those below 2^-126 as multiples of
+ * 2^-133).  A row that sees nothing (or whose scores are all -inf) has out = 0 and
  * lse = -inf.  What a row does not see does not reach it, NaN, infinities and any scale
- * included.
+ * included.  An infinite value reaches the rows that see it with a weight of 2^-100 of their
+ * largest or more; with less (a score of -inf, say) it makes NaN or counts as not seen.
  *
  *   q, out       [n, q_heads, head_dim], type VT_BF16 or VT_F32; n <= n_requests * max_rows
  *   page_table   [n_requests, table_pages] int32; entries past a request's tokens are

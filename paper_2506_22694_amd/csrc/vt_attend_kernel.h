@@ -82,7 +82,7 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 // Eight fp32 values (none -0) as the sum of three operands: the leading 8 bits of what is just below the value, those of what is just below the
 // rest, and the rest, which has 8.  (Below it by the last of its 24 bits; below an infinity are the largest finite ones.  0 is three zeros.)
-// Two terms: the rest is rounded, 2^-17 of the value at most, and is not zero either.
+// Two terms: the rest, of up to 2^-7 of the value, is rounded to 8 bits (2^-16 of the value at most), and is not zero either.
 template <int TERMS, typename Terms>
 __device__ __forceinline__ void split_terms(float (&v)[8], Terms &terms) {
 #pragma unroll

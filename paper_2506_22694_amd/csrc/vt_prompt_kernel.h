@@ -10,8 +10,8 @@
 //
 // 16 bytes c of token t lie at place c ^ key(t) of the token's row in LDS, so that the sixteen lanes that read sixteen rows use all of its 64 banks.
 //
-// A weight p goes into the product as two bf16 terms, 16 bits of it (one term, 8 bits, would be as large an error as the result's own rounding; the third,
-// which attention of few rows has, is 2^-8 of an error that the rounding of bf16 results hides already).
+// A weight p goes into the product as two bf16 terms, 16 bits of it, off by 2^-16 at most (one term, 8 bits, would be as large an error as the result's own rounding,
+// 2^-8; the third, which attention of few rows has, is 2^-8 of an error that the rounding of bf16 results hides already).
 //
 // 8192 rows of 32 heads of 128 values over 8, a window of 4096 in bf16: 585 us, 705 TFLOP/s; a tile of a wave is 96 matrix instructions and 314 others, which do not
 // overlap on a SIMD and take 93 % of its cycles.  64 query rows a workgroup where 128 are too few of them (one chunk of 256 rows, split as well).

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2506_22694_amd as vt
-from test_gpu_attention import BF16, _gen
+from test_gpu_attention import BF16, E4M3, _gen
 from test_gpu_four_bits import E2M1
 from test_gpu_window_attention import WIDE, case, check
 
@@ -110,3 +110,63 @@ def test_infinities_at_scores_of_minus_infinity_beside_a_window(hq, hk, D, rows)
     for got in out[:-1]:
         assert torch.equal(got[0][whole], out[-1][0][whole]) and torch.equal(got[1][whole], out[-1][1][whole])
     assert out[-1][0][whole].isfinite().all() and out[-1][1][whole].isfinite().all() and whole.sum() > 0.99 * whole.numel()
+
+
+@pytest.mark.parametrize("held", [BF16, E4M3, E2M1])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows", [2, 130])
+def test_bits_of_weights(held, D, rows):
+    """A token of weight 1 and value -3/4 beside one of weight w, about 3/4, and value 1: (w - 3/4) / (1 + w) is small, and has w's error whole.  Chunks, and bf16
+    rows over 4 bits, hold a weight as 8 bits that are cut off and a rest below 2^-7 of it that is rounded to 8: off by 2^-16 at most.  Others hold 24 bits.  fp32's part: z is
+    a sum of two products, exp2 and the sums are off by some half steps of 2^-24: 2^-20 covers 16."""
+    hk, length = 96, 700
+    cache, table, lengths, q, starts = case(_gen(D), held, BF16, hk, hk, D, 16, [length], rows=[rows])
+    page_a, at_a = table[0, 300 // 16].long(), 300 % 16
+    page_b, at_b = table[0, 411 // 16].long(), 411 % 16
+    one, small = {BF16: (1.0, 0.75), E4M3: (0x38, 0x34), E2M1: (4, 3)}[held]      # (4 bits: of a scale of 1/2)
+    if held == BF16:
+        k, v = cache.k, cache.v
+    else:
+        k, v = torch.zeros(2, *cache.k.shape[:3], D, dtype=torch.uint8, device="cuda").unbind(0)
+        for s in (cache.k_scale, cache.v_scale):
+            s.fill_(127 if held == E4M3 else 126)
+    k.zero_(), v.zero_()
+    k[..., 0] = one      # all other tokens: far below
+    k[page_a, :, at_a] = 0
+    k[page_b, :, at_b] = 0
+    k[page_b, :, at_b, 1] = k[page_b, :, at_b, 2] = one
+    v[page_a, :, at_a] = -small if held == BF16 else small + (0x80 if held == E4M3 else 8)
+    v[page_b, :, at_b] = one
+    if held == E4M3:
+        cache.k.view(torch.uint8).copy_(k), cache.v.view(torch.uint8).copy_(v)
+    elif held == E2M1:
+        for x, y in ((cache.k, k), (cache.v, v)):
+            x.view(torch.uint8).copy_(y[..., ::2] + 16 * y[..., 1::2])
+    q.zero_()
+    q[..., 0] = -4000.0
+    q[..., 1] = math.log2(0.75)
+    q[..., 2] = (torch.rand(q.shape[:2], generator=_gen(D + 1), device="cuda") * 2 - 1) * 2.0 ** -7
+    w = torch.exp2(q[..., 1].double() + q[..., 2].double())[..., None]
+    want = (w - 0.75) / (1 + w)
+    out, lse = vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=rows, window=length, scale=math.log(2.0), return_lse=True)
+    error = (2.0 ** -16 if rows > 2 or held == E2M1 else 0.0) + 2.0 ** -20
+    half = torch.ldexp(torch.ones_like(want), torch.frexp(want).exponent - 9)      # of a step of bf16 at the value itself
+    assert ((out.double() - want).abs() - half - error * w / (1 + w)).max().item() <= 0.0
+    assert (lse.double() - torch.log1p(w[..., 0])).abs().max().item() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("byte", [0, 1, 2, 3, 120, 246])
+@pytest.mark.parametrize("hk,D", [(256, 64), (96, 128), (200, 256)])
+def test_values_of_eight_bits_in_chunks_are_those_of_bf16(byte, hk, D):
+    """Each row sees its own token alone: what 8 bits hold of it, rounded to bf16 (below 2^-126 to multiples of 2^-133)."""
+    rows = 130
+    cache, table, lengths, q, starts = case(_gen(D), E4M3, BF16, hk, hk, D, 16, [700], rows=[rows])
+    codes = torch.arange(256, device="cuda", dtype=torch.uint8)
+    codes = codes[(codes & 0x7F) != 0x7F][:254]
+    cache.v.view(torch.uint8).copy_(codes[torch.randint(0, 254, cache.v.shape, generator=_gen(byte), device="cuda")])
+    cache.v_scale.fill_(byte)
+    out = vt.paged_attention(q, cache, table, lengths, row_start=starts, max_rows=rows, window=1)
+    slots = cache.slots(table, torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.arange(700 - rows, 700, device="cuda"))
+    held = cache.v.view(torch.uint8).transpose(1, 2).reshape(-1, hk, D)[slots].view(E4M3).double() * 2.0 ** (byte - 127)
+    assert torch.equal(out, held.float().to(BF16))
+    assert torch.equal(out, vt.kv_cache_read(cache, slots)[1])
