@@ -251,14 +251,15 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttendArgs a) {
                     z[j / 4][j % 4] = seen ? z[j / 4][j % 4] : kNone;
                 }
             }
-            // (a maximum that is left behind by no more than 2^kLag stays the base: weights of up to that are as exact, and little is rescaled)
-            constexpr float kLag = 8.0f;
+            // (the base is 2^kAhead above the maximum where it is set, and stays as long as no score passes it: little is rescaled, and no weight is above 1, which
+            // would make infinities of the largest values)
+            constexpr float kAhead = 8.0f;
             float most = kNone;
 #pragma unroll
             for (int j = 0; j < 4 * PIECES; ++j) most = fmaxf(most, z[j / 4][j % 4]);
             most = row_max(most) * scale_by;
-            if (__any(most > top[nt] + kLag)) {
-                const float now = fmaxf(top[nt], most), fade = top[nt] == kNone ? 0.0f : __builtin_amdgcn_exp2f(top[nt] - now);
+            if (__any(most > top[nt])) {
+                const float now = fmaxf(top[nt], most + kAhead), fade = top[nt] == kNone ? 0.0f : __builtin_amdgcn_exp2f(top[nt] - now);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
 #pragma unroll

@@ -170,3 +170,33 @@ def test_values_of_eight_bits_in_chunks_are_those_of_bf16(byte, hk, D):
     held = cache.v.view(torch.uint8).transpose(1, 2).reshape(-1, hk, D)[slots].view(E4M3).double() * 2.0 ** (byte - 127)
     assert torch.equal(out, held.float().to(BF16))
     assert torch.equal(out, vt.kv_cache_read(cache, slots)[1])
+
+
+@pytest.mark.parametrize("held", [BF16, E4M3, E2M1])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("rows", [2, 130])
+@pytest.mark.parametrize("later", [0, 3, 7, 9, 40])
+def test_the_largest_values(held, D, rows, later):
+    """A token of values of 2^125, its score log 2 times `later` above all others': results of no more than that, whatever base the weights are counted from."""
+    hk, length = 96, 700
+    cache, table, lengths, q, starts = case(_gen(D), held, BF16, hk, hk, D, 16, [length], rows=[rows])
+    page, place = table[0, 411 // 16].long(), 411 % 16
+    for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        (x if held == BF16 else x.view(torch.uint8)).zero_()
+        if s is not None:
+            s.fill_(127)
+    if held == BF16:
+        cache.k[page, :, place, 0] = 1.0
+        cache.v[page, :, place] = 2.0 ** 125
+    elif held == E4M3:
+        cache.k.view(torch.uint8)[page, :, place, 0] = 0x38
+        cache.v.view(torch.uint8)[page, :, place] = 0x38
+        cache.v_scale[page, :, place] = 252
+    else:
+        cache.k.view(torch.uint8)[page, :, place, 0] = 2
+        cache.v.view(torch.uint8)[page, :, place] = 0x22
+        cache.v_scale[page, :, :, place] = 252
+    q.zero_()
+    q[..., 0] = later
+    out, lse = check(cache, table, lengths, q, starts, length, 0, scale=math.log(2.0))
+    assert out.isfinite().all() and out[0, 0, 0] >= 2.0 ** 115
