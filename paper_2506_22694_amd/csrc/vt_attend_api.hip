@@ -98,8 +98,19 @@ constexpr int64_t kAttendOneTile = 1100000, kAttendOneTileOf16Bits = 1000000;
 // over a window of 512, 1280 steps, 18.6 us and 20.4, of 48, 1920 steps, 30.8 and 20.5; four of 24 over 2000, 1632 steps, 27.8 and 25.2; one of 512 over 4096 109
 // and 73, eight of 128 140 and 117.  8 bits, whose tiles are less to read again: two of 64 over 2000, 2176 steps, 24.9 and 28.9, eight of 64 over 512, 2560 steps,
 // 27.6 and 23.3.  28 heads of 64 values over 4, whose steps are of 64 query rows, bf16: two of 128 over 512, 672 steps, 13.8 and 16.1, one over 2000, 952 steps,
-// 21.9 and 20.4; 4 bits 14.9 and 19.5, 22.5 and 22.8.  A chunk in one share, 512 rows of one request: 109 us.)
-constexpr int64_t kPromptRows = 64, kPromptSteps = 2400, kPromptStepsOf16Bits = 1600, kPromptStepsOf64 = 700, kPromptWorkgroups = 512, kPromptTiles = 6;
+// 21.9 and 20.4; 8 bits 14.7 and 17.2, 22.9 and 21.1; 4 bits, which are more instructions to bring into LDS, 14.9 and 19.2, 22.5 and 22.6, eight of 128 rows of 8 heads over 512, 768
+// steps, 15.1 and 22.0, 12 heads over 3, four of 200 over 1024, 1560 steps, 26.5 and 22.4, eight of 256 over 400, 2304 steps, 26.8 and 19.4.  Heads past 128 values, whose steps are of 16
+// query rows and whose tiles of 32 tokens, 16 of 256 over 4, bf16: one of 128 over 1024, 1280 steps, 24.0 and 27.4, four of 64, 2304 steps, 43.2 and 30.5, one of 512 over 4096 196 and
+// 89; 8 bits, which attend_kernel has fewer registers for: four of 64 32.4 and 34.1, two of 256 over 2000, 9216 steps, 46.4 and 64.1, 32 over 8 of as many, 18432 steps, 70.6 and 102,
+// four of 512 over 1024, 26624 steps, 104 and 92, 32 over 8, 53248 steps, 211 and 168; 4 bits 57 and 67, 83 and 108, 112 and 96, 191 and 179.  Steps say no more than about what a
+// kernel takes: next to a line either one may lose a fifth, few heads of 64 values in bf16 and 8 bits a third (eight of 128 rows of 8 heads over 512 13.8 and 18.1).  A chunk in one
+// share, 512 rows of one request: 109 us.)
+constexpr int64_t kPromptRows = 64, kPromptSteps = 2400, kPromptStepsOf16Bits = 1600, kPromptStepsOf64 = 700, kPromptStepsOf64In4Bits = 2000, kPromptStepsPast128 = 24000,
+                  kPromptWorkgroups = 512, kPromptTiles = 6;
+int64_t prompt_steps_from(int D, int cache_type) {
+    if (D <= 64) return cache_type == VT_E2M1 ? kPromptStepsOf64In4Bits : kPromptStepsOf64;
+    return cache_type == VT_BF16 ? kPromptStepsOf16Bits : D <= 128 ? kPromptSteps : kPromptStepsPast128;
+}
 
 Split split_of(int64_t n, int q_heads, int kv_heads, int D, int requests, int max_rows, int64_t max_length, bool f32, int cache_type,
                bool windowed = false) {
@@ -189,7 +200,7 @@ int attention(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_he
     Split split = split_of(n, q_heads, cache->heads, cache->head_dim, n_requests, max_rows, seen, f32, cache->type, window > 0);
     const bool prompt = split.ok && window > 0 && tail_mask == nullptr && !f32 && chunk > kPromptRows &&
                         prompt_steps(chunk, cache->head_dim) * cache->heads * n_requests * ((seen + vt::kAttendStep - 1) / vt::kAttendStep) >=
-                            (cache->head_dim <= 64 ? kPromptStepsOf64 : cache->type == VT_BF16 ? kPromptStepsOf16Bits : kPromptSteps);
+                            prompt_steps_from(cache->head_dim, cache->type);
     if (prompt) split = split_of_prompt(chunk, n_requests, cache->heads, cache->head_dim, seen, max_length);
     if (!split.ok || table_pages < 1 || !std::isfinite(scale)) return VT_ERR_SHAPE;
     if (row_start == nullptr && (n != n_requests || max_rows != 1)) return VT_ERR_SHAPE;

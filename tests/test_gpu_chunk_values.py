@@ -12,6 +12,9 @@ from test_gpu_window_attention import WIDE, case, check
 
 pytestmark = pytest.mark.gpu
 
+# Chunks of enough work go through a kernel of their own: over 8 and 4 bits, heads past 128 values do with many kv heads
+PAST_128 = [(512, 512, 256), (320, 320, 160), (448, 224, 192)]
+
 
 def hold(cache, table, token, head, d, value, b=0):
     """An infinity (4 bits: a group of zeros beside it, 6 or -6 at a scale of 2^127) or NaN as value d of a token's row."""
@@ -20,6 +23,10 @@ def hold(cache, table, token, head, d, value, b=0):
         cache.v[page, head, place, d] = value
         return
     codes = cache.v.view(torch.uint8)[page, head, place]
+    if cache.v.dtype == E4M3:
+        assert math.isnan(value)
+        codes[d] = 0x7F
+        return
     group = d // 32
     codes[16 * group:16 * group + 16] = 0
     codes[d // 2] = (0xF if value < 0 else 7) << 4 * (d % 2)
@@ -27,7 +34,7 @@ def hold(cache, table, token, head, d, value, b=0):
 
 
 @pytest.mark.parametrize("held", [BF16, E2M1])
-@pytest.mark.parametrize("hq,hk,D", WIDE)
+@pytest.mark.parametrize("hq,hk,D", WIDE + PAST_128)
 def test_infinities_that_every_row_sees(held, hq, hk, D):
     """Rows of q = 0 have weights of 1, of which bf16 holds all; other rows a token of weight 1 where the largest score's is."""
     g = _gen(hq + D)
@@ -38,8 +45,10 @@ def test_infinities_that_every_row_sees(held, hq, hk, D):
     hold(cache, table, 330, hk - 1, 9, math.nan)
     hold(cache, table, 223, 2, 1, math.inf, 1)
     hold(cache, table, 222, 2, 1, math.inf, 1)
-    if held == BF16:      # the largest score of a row of each kv head
-        cache.k[table[0, 350 // 16].long(), :, 350 % 16] = 2.0 * q[1].view(hk, -1, D)[:, 0]
+    if held == BF16:
+        # the largest score of a row of each kv head, x |q|^2 / sqrt(D), |q|^2 = 2.25 D or so: of 256 values 52 at x = 1 (104 at x = 2) times log 2, and the
+        # infinities' weights 2^-52 of its own (2^-104, less than what reaches a row)
+        cache.k[table[0, 350 // 16].long(), :, 350 % 16] = (2.0 if D <= 160 else 1.0) * q[1].view(hk, -1, D)[:, 0]
     for window, sinks in ((600, 0), (500, 40), (1 << 30, 0)):
         out, lse = check(cache, table, lengths, q, starts, window, sinks)
         G = hq // hk
@@ -67,7 +76,7 @@ def test_infinities_in_a_share_of_a_chunk(held, hq, hk, D):
 def test_infinities_of_small_weights(held, D, rows):
     """Weights that are powers of two, down to 2^-100 of the row's largest: scores are whole numbers times log 2."""
     g = _gen(D)
-    hk = 96
+    hk = 96 if D <= 128 else 512
     cache, table, lengths, q, starts = case(g, held, BF16, hk, hk, D, 16, [700], rows=[rows])
     assert float(torch.tensor(math.log(2.0), dtype=torch.float32) * torch.tensor(1.4426950408889634, dtype=torch.float32)) == 1.0
     q.zero_()
@@ -119,7 +128,7 @@ def test_bits_of_weights(held, D, rows):
     """A token of weight 1 and value -3/4 beside one of weight w, about 3/4, and value 1: (w - 3/4) / (1 + w) is small, and has w's error whole.  Chunks, and bf16
     rows over 4 bits, hold a weight as 8 bits that are cut off and a rest below 2^-7 of it that is rounded to 8: off by 2^-16 at most.  Others hold 24 bits.  fp32's part: z is
     a sum of two products, exp2 and the sums are off by some half steps of 2^-24: 2^-20 covers 16."""
-    hk, length = 96, 700
+    hk, length = 96 if D <= 128 else 512, 700
     cache, table, lengths, q, starts = case(_gen(D), held, BF16, hk, hk, D, 16, [length], rows=[rows])
     page_a, at_a = table[0, 300 // 16].long(), 300 % 16
     page_b, at_b = table[0, 411 // 16].long(), 411 % 16
@@ -156,10 +165,9 @@ def test_bits_of_weights(held, D, rows):
 
 
 @pytest.mark.parametrize("byte", [0, 1, 2, 3, 120, 246])
-@pytest.mark.parametrize("hk,D", [(256, 64), (96, 128), (200, 256)])
-def test_values_of_eight_bits_in_chunks_are_those_of_bf16(byte, hk, D):
+@pytest.mark.parametrize("hk,D,rows", [(256, 64, 130), (96, 128, 130), (512, 256, 300)])
+def test_values_of_eight_bits_in_chunks_are_those_of_bf16(byte, hk, D, rows):
     """Each row sees its own token alone: what 8 bits hold of it, rounded to bf16 (below 2^-126 to multiples of 2^-133)."""
-    rows = 130
     cache, table, lengths, q, starts = case(_gen(D), E4M3, BF16, hk, hk, D, 16, [700], rows=[rows])
     codes = torch.arange(256, device="cuda", dtype=torch.uint8)
     codes = codes[(codes & 0x7F) != 0x7F][:254]
@@ -178,7 +186,7 @@ def test_values_of_eight_bits_in_chunks_are_those_of_bf16(byte, hk, D):
 @pytest.mark.parametrize("later", [0, 3, 7, 9, 40])
 def test_the_largest_values(held, D, rows, later):
     """A token of values of 2^125, its score log 2 times `later` above all others': results of no more than that, whatever base the weights are counted from."""
-    hk, length = 96, 700
+    hk, length = 96 if D <= 128 else 512, 700
     cache, table, lengths, q, starts = case(_gen(D), held, BF16, hk, hk, D, 16, [length], rows=[rows])
     page, place = table[0, 411 // 16].long(), 411 % 16
     for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
@@ -200,3 +208,30 @@ def test_the_largest_values(held, D, rows, later):
     q[..., 0] = later
     out, lse = check(cache, table, lengths, q, starts, length, 0, scale=math.log(2.0))
     assert out.isfinite().all() and out[0, 0, 0] >= 2.0 ** 115
+
+
+@pytest.mark.parametrize("hq,hk,D", PAST_128)
+@pytest.mark.parametrize("held", [E4M3, E2M1])
+def test_chunks_of_heads_past_128_values(held, hq, hk, D):
+    a = case(_gen(hq + D), held, BF16, hq, hk, D, 64, [400, 390, 700, 70, 65], rows=[200, 1, 97, 70, 100])
+    for window, sinks in ((1, 0), (7, 2), (33, 0), (100, 20), (1 << 30, 0), (3, 1 << 30)):
+        check(*a, window, sinks)
+    for scale in (0.0, -0.2):
+        check(*a, 100, 4, scale=scale)
+    # ... some of which only some rows see
+    cache, table = a[:2]
+    hold(cache, table, 260, 0, 5, math.nan)
+    hold(cache, table, 350, hk - 1, D - 3, math.nan)
+    hold(cache, table, 630, 3, 9, math.nan, 2)
+    for window, sinks in ((100, 20), (1 << 30, 0)):
+        out, _ = check(*a, window, sinks)
+        assert out[:30].isfinite().all() and out.isnan().any()
+
+
+def test_a_long_chunk_of_heads_past_128_values_in_shares():
+    for held in (E4M3, E2M1):
+        a = case(_gen(8), held, BF16, 8, 2, 256, 64, [30000, 9000], rows=[200, 130])
+        for window, sinks in ((29000, 4), (1 << 30, 0)):
+            out, lse = check(*a, window, sinks)
+            again = vt.paged_attention(a[3], *a[:3], row_start=a[4], max_rows=200, window=window, sinks=sinks, return_lse=True)
+            assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
