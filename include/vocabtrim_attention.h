@@ -190,7 +190,8 @@ size_t vt_paged_attention_ws_bytes(int64_t n, int32_t q_heads, int32_t kv_heads,
  *                 prompt's length plus their depth); one below lengths[b] - 64 counts as that.
  *                 NULL: a request's R rows are its last tokens, p = lengths[b] - R + (0 .. R - 1)
  *                 (R: at most max_rows)
- *   window        1 .. 2^30; from max_length on: every token up to the row's own
+ *   window        1 .. 2^30; from max_length on: every token up to the row's own (a causal prompt's
+ *                 chunk on a layer without a window: vt_paged_attention has its rows see later rows' tokens)
  *   sinks         0 .. 2^30
  * Workspace as for vt_paged_attention with the same sizes. */
 int vt_paged_attention_window(const void *q, int64_t q_stride, int type, int64_t n, int32_t q_heads, const vt_kv_cache *cache,

@@ -350,6 +350,9 @@ def paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, l
     some row sees.  A request's rows are its last tokens and, without a tail mask, see none behind themselves: a prompt's chunk
     whose keys are cached.  With a tail mask the nodes of a tree may have `positions` (int32 or int64 [n]; the prompt's length plus
     their depth), which count from the first of the last 64 tokens on.  A window of max_length and more: all tokens up to the row's own.
+
+    Without a window a row sees all cached tokens of its request that no tail mask hides, those of the request's later rows too: a causal
+    prompt on a layer without a window is window=max_length.
     A q that requires a gradient is refused: there is none."""
     L = load_library()
     if binding._bind is not None and type(ws) is AttentionWorkspace and type(cache) is KVCache:
