@@ -29,7 +29,7 @@
 //
 // 131001 tokens of one request, 8 kv heads of 128 values in bf16, 4 query heads each: 537 MB in 80 us, 6.7 TB/s, where a plain read of as much
 // takes 79; 224 vector and 32 matrix instructions a tile (8 bits: 317 and 32; 48 ragged requests 541 MB in 95 us, 5.7 TB/s).  4 bits: 143 MB in 34 us,
-// 48 ragged requests 292 MB in 60, 4.8 TB/s: 262 and 24 instructions a tile, which do not overlap on a SIMD, are what it takes.
+// 48 ragged requests 292 MB in 60, 4.8 TB/s: 262 and 24 instructions a tile, which hardly overlap on a SIMD, are most of it.
 #pragma once
 #include "vt_values.h"
 

@@ -8,13 +8,15 @@
 //   out^T [d, row] = V^T p^T           V's operand: four tokens of one column in a lane, by the transposing read of LDS; p's operand is what the
 //                                      first product leaves in a lane, so the running maxima and sums are a lane's own
 //
-// 16 bytes c of token t lie at place c ^ key(t) of the token's row in LDS, so that the sixteen lanes that read sixteen rows use all of its 64 banks.
+// 16 bytes c of token t lie at place c ^ key(t) of the token's row in LDS, so that the sixteen lanes that read sixteen rows of K use all of its 64 banks.  (The transposing reads
+// of V meet in banks: 24 % of LDS's cycles are conflicts, 38 % with 64-value heads.)
 //
 // A weight p goes into the product as two bf16 terms, 16 bits of it, off by 2^-16 at most (one term, 8 bits, would be as large an error as the result's own rounding,
 // 2^-8; the third, which attention of few rows has, is 2^-8 of an error that the rounding of bf16 results hides already).
 //
-// 8192 rows of 32 heads of 128 values over 8, a window of 4096 in bf16: 585 us, 705 TFLOP/s; a tile of a wave is 96 matrix instructions and 314 others, which do not
-// overlap on a SIMD and take 93 % of its cycles.  64 query rows a workgroup where 128 are too few of them (one chunk of 256 rows, split as well).
+// 8192 rows of 32 heads of 128 values over 8, a window of 4096 in bf16: 575 to 595 us, 695 to 718 TFLOP/s, once the card's clock has settled (the first some fifty calls after other
+// work 660 to 810); a tile of a wave is 96 matrix instructions and some 310 others, which hardly overlap on a SIMD (a wave of products beside one of multiply-adds: 95 % of the sum
+// of both) and take 90 % of its cycles.  64 query rows a workgroup where 128 are too few of them (one chunk of 256 rows, split as well).
 #pragma once
 #include "vt_attend_kernel.h"
 
